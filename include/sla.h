@@ -51,10 +51,12 @@ extern "C" {
 #define SLA_ERR_DTYPE (-3)       /* unknown activation dtype               */
 #define SLA_ERR_TOPOLOGY (-4)    /* parent array not in topological order  */
 #define SLA_ERR_PATH (-5)        /* accepted path is not a root path       */
-#define SLA_ERR_ALIAS (-6)       /* pending factors overlap output factors */
+#define SLA_ERR_ALIAS (-6)       /* an output overlaps a buffer the call reads */
 #define SLA_ERR_UNSUPPORTED (-7) /* valid request the library cannot run  */
 #define SLA_ERR_HIP (-8)         /* the HIP runtime reported an error      */
 #define SLA_ERR_SCORE (-9)       /* a draft log-probability above 0 or NaN */
+#define SLA_ERR_PAGE (-10)       /* a page number outside the pool         */
+#define SLA_ERR_LENGTH (-11)     /* a cache length or row count out of range */
 
 /* Activation dtypes of q, k, v (and of the stored k factor). */
 #define SLA_DTYPE_F32 0
@@ -368,6 +370,148 @@ int sla_tree_mask_to_parent(const uint64_t *mask, int32_t batch, int32_t n_nodes
 /* Host version for one mask: returns SLA_OK, SLA_ERR_NULL, SLA_ERR_SHAPE or
  * SLA_ERR_TOPOLOGY. */
 int sla_tree_mask_to_parent_host(const uint64_t *mask, int32_t n_nodes, int32_t *parent);
+
+/* ---------------------------------------- attention over a paged cache
+ *
+ * The hybrid models that SpecLA's targets belong to interleave their
+ * recurrent layers with attention layers.  For one of these, a speculative
+ * round is: the draft's keys and values enter the cache behind the committed
+ * tokens (sla_attn_append, which also normalises and rotates queries and
+ * keys), every node attends to the committed tokens and to its own root path
+ * (sla_attn_verify), and the accepted path's rows move together behind the
+ * committed tokens (sla_attn_commit).  A 1-node draft is the decode step.  A
+ * prompt is a batch of 64-node chains that share one page-table row, the
+ * chunk c with cache_len 64 c: append all of them, then verify all of them.
+ *
+ * Cache.  Keys and values lie in two pools of pages,
+ *     [layers][n_pages][kv_heads][page_size][head_dim]
+ * in the activation dtype; sla_attn_append and sla_attn_verify are given one
+ * layer's.  Row r of sequence b is row r mod page_size of page
+ * page_table[b][r / page_size], in every head; rows 0..cache_len[b]-1 are the
+ * committed tokens and row cache_len[b] + j is draft node j's.  Entries of
+ * the page table past a sequence's last row are not read.  Sequences may share
+ * pages; no two of one call may write the same row.
+ *
+ * Positions.  Node j stands at position cache_len[b] + depth(j) - 1, depth as
+ * in sla_topology (a root has depth 1): siblings share a position.
+ *
+ * Data errors of a sequence (status[b]): SLA_ERR_TOPOLOGY; SLA_ERR_LENGTH if
+ * cache_len[b] < 0, cache_len[b] + n_nodes > max_pages page_size or
+ * cache_len[b] > max_len; SLA_ERR_PAGE if a page it needs is not in
+ * [0, n_pages).  Its cache is then untouched and its outputs are unspecified;
+ * no memory outside the given buffers is accessed. */
+typedef struct sla_attn_shape {
+  int32_t batch;     /* B >= 1                                              */
+  int32_t q_heads;   /* a multiple of kv_heads; query head h reads the kv
+                        head h / (q_heads / kv_heads)                       */
+  int32_t kv_heads;  /* >= 1                                                */
+  int32_t head_dim;  /* D: 64, 128 or 256                                   */
+  int32_t n_nodes;   /* draft nodes per sequence, 1..SLA_MAX_NODES          */
+  int32_t qkv_dtype; /* SLA_DTYPE_F32 or SLA_DTYPE_BF16: activations, cache
+                        and output                                          */
+  int32_t topology;  /* SLA_TOPO_TREE or SLA_TOPO_CHAIN                     */
+  int32_t page_size; /* rows of a page: 16, 32, 64, 128 or 256              */
+  int32_t n_pages;   /* pages of the pool                                   */
+  int32_t max_pages; /* entries of a page-table row; max_pages page_size
+                        < 2^31                                              */
+  int32_t max_len;   /* promise that cache_len[b] <= max_len, by which
+                        sla_attn_verify lays out its work; 0: none, the
+                        page table's capacity                               */
+} sla_attn_shape;
+
+#define SLA_ROPE_HALF 0        /* pairs (x[i], x[i + rope_dim / 2])          */
+#define SLA_ROPE_INTERLEAVED 1 /* pairs (x[2 i], x[2 i + 1])                 */
+
+/* What sla_attn_append does to queries and keys, head by head:
+ *     y = x rsqrt(mean(x^2) + eps) w      (w: q_norm or k_norm; NULL: y = x)
+ * in fp32, then each pair i of the first rope_dim elements is turned,
+ *     (a, b) -> (a cos - b sin, b cos + a sin),
+ * by the angle whose cosine and sine the table holds for the node's position:
+ *     rope[pos][i] = cos, rope[pos][rope_dim / 2 + i] = sin.
+ * Scalings for long contexts are the table's matter.  Results are rounded once
+ * to the activation dtype.  Values are stored as they are. */
+typedef struct sla_attn_transform {
+  const float *q_norm; /* device fp32 [D] or NULL                            */
+  const float *k_norm; /* device fp32 [D] or NULL                            */
+  float eps;           /* >= 0                                               */
+  const float *rope;   /* device fp32 [rope_len][rope_dim], NULL if rope_dim
+                          is 0                                               */
+  int32_t rope_dim;    /* 0 (no rotation) or a multiple of 16 up to D        */
+  int32_t rope_len;    /* positions of the table; a node past them is
+                          SLA_ERR_LENGTH                                     */
+  int32_t layout;      /* SLA_ROPE_HALF or SLA_ROPE_INTERLEAVED              */
+} sla_attn_transform;
+
+/* sla_attn_append -- the draft's queries, normalised and rotated, to q_out,
+ * and its keys (likewise) and values to the cache rows cache_len[b] + j.
+ *   q [B][n][q_heads][D], k, v [B][n][kv_heads][D] in the activation dtype;
+ *     a node's heads are dense and consecutive nodes lie *_stride elements
+ *     apart (q_heads D or kv_heads D if dense, the projection's width where
+ *     all three are parts of one fused projection); strides are multiples of
+ *     16 bytes.
+ *   transform  norms and rotation; NULL: neither.
+ *   parent_idx device int32 [B][n]; page_table [B][max_pages]; cache_len [B].
+ *   q_out      device [B][n][q_heads][D]; must not overlap q, k or v.
+ *   k_cache, v_cache  device [n_pages][kv_heads][page_size][D].
+ *   status     device int32 [B] or NULL.
+ * max_len is ignored. */
+int sla_attn_append(const sla_attn_shape *shape, const sla_attn_transform *transform, const void *q,
+                    int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                    const int32_t *parent_idx, const int32_t *page_table, const int32_t *cache_len,
+                    void *q_out, void *k_cache, void *v_cache, int32_t *status, hipStream_t stream);
+
+/* sla_attn_verify -- attention of every draft node, for all sequences:
+ *     o_j = sum_i p_ji v_i,  p_j = softmax_i(scale q_j . k_i),
+ * i over the committed rows and the rows of the nodes on j's root path (j
+ * included), which sla_attn_append has written.  Rows of other nodes and rows
+ * past the draft have no part in o_j, whatever they hold (infinities and NaN
+ * included).  Scores, the softmax's running maximum and sum, and the outputs
+ * are held in fp32; bf16 activations round the weights p to bf16 for the
+ * matrix cores, fp32 ones are multiplied exactly.
+ *   q, out  device [B][n][q_heads][D], activation dtype; they must not overlap.
+ *   k_cache, v_cache  device [n_pages][kv_heads][page_size][D].
+ *   workspace  device memory of at least sla_attn_workspace_bytes(shape)
+ *           bytes (may be NULL if that is 0), 16-byte aligned, used until the
+ *           call's work has finished; it needs no initialisation.
+ *   status  device int32 [B] or NULL. */
+int sla_attn_verify(const sla_attn_shape *shape, float scale, const void *q, const void *k_cache,
+                    const void *v_cache, const int32_t *parent_idx, const int32_t *page_table,
+                    const int32_t *cache_len, void *out, void *workspace, size_t workspace_bytes,
+                    int32_t *status, hipStream_t stream);
+
+/* Bytes of sla_attn_verify's workspace for this shape on the current device
+ * (0 on a bad shape). */
+size_t sla_attn_workspace_bytes(const sla_attn_shape *shape);
+
+/* sla_attn_commit -- the accepted path's rows of every layer move to the rows
+ * cache_len[b] + t, t = 0..len[b]-1, in one call (bit for bit; rows that are
+ * in place stay).
+ *   k_cache, v_cache  device [layers][n_pages][kv_heads][page_size][D].
+ *   parent_idx  the draft's parent array, device int32 [B][n].
+ *   path, len   as in sla_pending: device int32 [B][n] (-1 padded) and [B].
+ *   new_len     device int32 [B] or NULL: cache_len[b] + len[b] (cache_len[b]
+ *               on an error).  It must not overlap cache_len, which the call
+ *               reads throughout.
+ *   status      device int32 [B] or NULL (also SLA_ERR_PATH).
+ * q_heads, topology and max_len are ignored. */
+int sla_attn_commit(const sla_attn_shape *shape, int32_t layers, void *k_cache, void *v_cache,
+                    const int32_t *parent_idx, const int32_t *path, const int32_t *len,
+                    const int32_t *page_table, const int32_t *cache_len, int32_t *new_len, int32_t *status,
+                    hipStream_t stream);
+
+/* sla_page_copy -- copy pages within the pools, all layers and heads: page
+ * dst[i] becomes page src[i], for i = 0..copies-1 (a sequence that forks off
+ * copies its last, partly filled page and shares the full ones).
+ *   rows    device int32 [copies] or NULL: only the first rows[i] rows of the
+ *           page, 0..page_size (else SLA_ERR_LENGTH).
+ *   src, dst device int32 [copies].  The pages of dst are distinct and none of
+ *           them is in src, unless src[i] = dst[i], which copies nothing.
+ *   status  device int32 [copies] or NULL: 0, SLA_ERR_PAGE or SLA_ERR_LENGTH
+ *           (then the page is untouched).
+ * Of the shape, kv_heads, head_dim, qkv_dtype, page_size and n_pages are used. */
+int sla_page_copy(const sla_attn_shape *shape, int32_t layers, void *k_cache, void *v_cache,
+                  const int32_t *src, const int32_t *dst, const int32_t *rows, int32_t copies,
+                  int32_t *status, hipStream_t stream);
 
 /* ------------------------------------------------------------ host helpers */
 

@@ -30,6 +30,8 @@ SLA_ERR_ALIAS = -6
 SLA_ERR_UNSUPPORTED = -7
 SLA_ERR_HIP = -8
 SLA_ERR_SCORE = -9
+SLA_ERR_PAGE = -10
+SLA_ERR_LENGTH = -11
 
 SLA_DTYPE_F32 = 0
 SLA_DTYPE_BF16 = 1
@@ -49,6 +51,9 @@ FAMILIES = {"gdn": SLA_FAMILY_GDN, "deltanet": SLA_FAMILY_DELTANET, "decay": SLA
 SLA_ACT_NONE = 0
 SLA_ACT_SILU = 1
 SLA_CONV_MAX_KERNEL = 4
+SLA_ROPE_HALF = 0
+SLA_ROPE_INTERLEAVED = 1
+ROPE_LAYOUTS = {"half": SLA_ROPE_HALF, "interleaved": SLA_ROPE_INTERLEAVED}
 
 ROUTES = {"auto": SLA_ROUTE_AUTO, "serial": SLA_ROUTE_SERIAL, "parallel": SLA_ROUTE_PARALLEL,
           "hybrid": SLA_ROUTE_HYBRID}
@@ -79,6 +84,19 @@ class SlaConvShape(ctypes.Structure):
 class SlaConvPending(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("parent", ctypes.c_void_p), ("n_nodes", ctypes.c_int32),
                 ("path", ctypes.c_void_p), ("len", ctypes.c_void_p)]
+
+
+class SlaAttnShape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("n_nodes", ctypes.c_int32), ("qkv_dtype", ctypes.c_int32),
+                ("topology", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class SlaAttnTransform(ctypes.Structure):
+    _fields_ = [("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("rope", ctypes.c_void_p), ("rope_dim", ctypes.c_int32), ("rope_len", ctypes.c_int32),
+                ("layout", ctypes.c_int32)]
 
 
 class SlaError(RuntimeError):
@@ -127,6 +145,19 @@ def lib():
         L.sla_tree_mask_to_parent.restype = ctypes.c_int
         L.sla_tree_mask_to_parent_host.argtypes = [vp, i32, vp]
         L.sla_tree_mask_to_parent_host.restype = ctypes.c_int
+        i64, size = ctypes.c_int64, ctypes.c_size_t
+        shape = ctypes.POINTER(SlaAttnShape)
+        L.sla_attn_append.argtypes = [shape, ctypes.POINTER(SlaAttnTransform), vp, i64, vp, i64, vp, i64, vp, vp, vp,
+                                      vp, vp, vp, vp, vp]
+        L.sla_attn_append.restype = ctypes.c_int
+        L.sla_attn_verify.argtypes = [shape, ctypes.c_float, vp, vp, vp, vp, vp, vp, vp, vp, size, vp, vp]
+        L.sla_attn_verify.restype = ctypes.c_int
+        L.sla_attn_workspace_bytes.argtypes = [shape]
+        L.sla_attn_workspace_bytes.restype = size
+        L.sla_attn_commit.argtypes = [shape, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.sla_attn_commit.restype = ctypes.c_int
+        L.sla_page_copy.argtypes = [shape, i32, vp, vp, vp, vp, vp, i32, vp, vp]
+        L.sla_page_copy.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -325,6 +356,65 @@ def sla_conv_commit(conv_state, x, parent_idx, path, length, *, kernel_size=None
         kernel_size = whole
     code = (_nat or native()).conv_commit(conv_state, x, parent_idx, path, length, kernel_size, status)
     _check(code, "sla_conv_commit")
+
+
+# ------------------------------------------- attention over a paged cache
+def sla_attn_append(q, k, v, parent_idx, page_table, cache_len, q_out, k_cache, v_cache, *, q_norm=None, k_norm=None,
+                    eps: float = 1e-6, rope=None, layout: str = "half", status=None, topology: str = "tree"):
+    """Enqueue a draft's entry into one layer's cache on the current stream
+    (see sla_attn_append in sla.h): its queries, normalised and rotated, to
+    q_out, its keys (likewise) and values to the cache rows behind cache_len.
+
+    q [B][n][Hq][D], k, v [B][n][Hkv][D], each node's heads dense and the nodes a
+    constant step apart (parts of one fused projection are taken as they are);
+    parent_idx [B][n], page_table [B][pages], cache_len [B] int32; q_out
+    [B][n][Hq][D]; k_cache, v_cache [pages][Hkv][page size][D]; q_norm, k_norm
+    [D] fp32 or None; rope [positions][rotated elements] fp32, cosines first
+    (see cache.rope_table), or None."""
+    code = (_nat or native()).attn_append(q, k, v, parent_idx, page_table, cache_len, q_out, k_cache, v_cache, q_norm,
+                                          k_norm, eps, rope, ROPE_LAYOUTS[layout], status, TOPOLOGIES[topology])
+    _check(code, "sla_attn_append")
+
+
+def attn_workspace(q, k_cache, page_table, *, max_len: int = 0):
+    """A workspace for sla_attn_verify calls with these shapes and max_len (None
+    if they need none).  One call uses it at a time."""
+    torch = _torch()
+    B, n, heads, _ = q.shape
+    nbytes = (_nat or native()).attn_workspace_bytes(B, n, heads, k_cache, page_table.shape[1], max_len)
+    return torch.empty(nbytes, dtype=torch.uint8, device=k_cache.device) if nbytes else None
+
+
+def sla_attn_verify(q, k_cache, v_cache, parent_idx, page_table, cache_len, out, *, scale: Optional[float] = None,
+                    max_len: int = 0, workspace=None, status=None, topology: str = "tree"):
+    """Enqueue the attention of every draft node over the committed rows and its
+    root path on the current stream (see sla_attn_verify in sla.h).
+
+    q, out [B][n][Hq][D]; k_cache, v_cache [pages][Hkv][page size][D] with the
+    draft appended; scale defaults to D^-0.5; max_len promises cache_len <=
+    max_len (0: the page table's capacity); workspace: from attn_workspace."""
+    if scale is None:
+        scale = q.shape[-1] ** -0.5
+    code = (_nat or native()).attn_verify(q, k_cache, v_cache, parent_idx, page_table, cache_len, out, scale, max_len,
+                                          workspace, status, TOPOLOGIES[topology])
+    _check(code, "sla_attn_verify")
+
+
+def sla_attn_commit(k_cache, v_cache, parent_idx, path, length, page_table, cache_len, *, new_len=None, status=None):
+    """Enqueue the move of the accepted paths' rows behind the committed ones, in
+    every layer of the cache, on the current stream (see sla_attn_commit in
+    sla.h).  k_cache, v_cache [layers][pages][Hkv][page size][D] (or one layer's);
+    new_len [B] int32 or None receives cache_len + length."""
+    code = (_nat or native()).attn_commit(k_cache, v_cache, parent_idx, path, length, page_table, cache_len, new_len,
+                                          status)
+    _check(code, "sla_attn_commit")
+
+
+def sla_page_copy(k_cache, v_cache, src, dst, *, rows=None, status=None):
+    """Enqueue page dst[i] = page src[i] (its first rows[i] rows) in every layer of
+    the cache on the current stream (see sla_page_copy in sla.h)."""
+    code = (_nat or native()).page_copy(k_cache, v_cache, src, dst, rows, status)
+    _check(code, "sla_page_copy")
 
 
 # ------------------------------------------------- draft pruning and packing

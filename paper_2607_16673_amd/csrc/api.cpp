@@ -14,7 +14,7 @@
 
 namespace {
 
-constexpr int kVersion = 20000;  // 2.0.0: the route moved into sla_shape
+constexpr int kVersion = 20100;  // 2.1.0: attention over a paged cache
 
 bool dk_ok(int dk) { return dk == 64 || dk == 128 || dk == 256; }
 
@@ -96,10 +96,12 @@ const char *sla_status_string(int status) {
     case SLA_ERR_DTYPE: return "unknown activation dtype";
     case SLA_ERR_TOPOLOGY: return "parent array is not in topological order";
     case SLA_ERR_PATH: return "accepted path is not a root path";
-    case SLA_ERR_ALIAS: return "pending factors overlap output factors";
+    case SLA_ERR_ALIAS: return "an output overlaps a buffer the call reads";
     case SLA_ERR_UNSUPPORTED: return "unsupported configuration";
     case SLA_ERR_HIP: return "HIP runtime error";
     case SLA_ERR_SCORE: return "draft log-probability above 0 or NaN";
+    case SLA_ERR_PAGE: return "page number outside the pool";
+    case SLA_ERR_LENGTH: return "cache length or row count out of range";
     default: return "unknown status";
   }
 }

@@ -1,0 +1,460 @@
+// attn_verify.hip -- attention of a draft's nodes over the paged cache:
+//     o_j = sum_i p_ji v_i,  p_j = softmax_i(scale q_j . k_i),
+// i over the committed rows and the nodes of j's root path.
+//
+// A kv head's queries are the rows r = node * G + g (G query heads to a kv
+// head): all of them read the same keys.  A workgroup takes up to 64 QT rows
+// of one kv head of one sequence and a range of its keys, walks the range in
+// tiles that it stages in LDS, and keeps the running maximum and sum of every
+// row's softmax, so that the keys and values are read once.  Where a launch
+// would have too few workgroups the keys are split over several; each then
+// leaves its unnormalised output and statistics in the workspace and a second
+// kernel joins them.
+//
+// On the matrix cores the scores are formed transposed, S^T = K Q^T: a lane
+// of v_mfma_f32_16x16x32_bf16 then holds four consecutive keys of one query,
+// which is what the B operand of O^T = V^T P^T takes, so the weights go from
+// one product to the next within the lane, and a row's statistics are one
+// value per lane.  V^T comes out of the row-major tile by ds_read_b64_tr_b16.
+// fp32 activations use v_mfma_f32_16x16x4_f32 in the same arrangement, with
+// exact products.
+#include <type_traits>
+
+#include "attn_device.hpp"
+
+namespace sla {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kQueries = 16;  // queries of one matrix tile
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+template <typename T, int D>
+struct Tile {
+  static constexpr bool kBf16 = sizeof(T) == 2;
+  static constexpr int kRow = D * (int)sizeof(T);  // bytes of a row
+  static constexpr int kKeys = 16384 / kRow;       // rows of a tile
+  // rows are padded so that a wave's fragment reads spread over the banks: 16
+  // rows a 16-byte step apart for K; for V four rows of 32 bytes each in bf16
+  static constexpr int kPitchK = kRow + 16;
+  static constexpr int kPitchV = kRow + (kBf16 ? 32 : 16);
+  static constexpr int kCols = kRow / 16;                // 16-byte pieces of a row
+  static constexpr int kPassRows = kThreads / kCols;     // rows one pass of the workgroup loads
+  static constexpr int kPasses = kKeys / kPassRows;
+  static constexpr int kBuffer = kKeys * (kPitchK + kPitchV);
+};
+
+struct Split {
+  int n;      // splits of every unit
+  int chunk;  // keys of a split, a multiple of the tile
+};
+
+// A query fragment: the B operand of S^T = K Q^T for 16 queries.
+template <typename T, int D>
+struct Frag;
+template <int D>
+struct Frag<bf16, D> {
+  bf16x8 x[D / 32];
+};
+template <int D>
+struct Frag<float, D> {
+  f32x4 x[D / 16];
+};
+
+// x without its infinite and NaN elements; `found` is set if there were any.
+__device__ __forceinline__ u32x4 finite_part(u32x4 x, bool &found, bf16) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool lo = (x[i] & 0x7f80u) == 0x7f80u, hi = (x[i] & 0x7f800000u) == 0x7f800000u;
+    found |= lo || hi;
+    x[i] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+  }
+  return x;
+}
+__device__ __forceinline__ u32x4 finite_part(u32x4 x, bool &found, float) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool bad = (x[i] & 0x7f800000u) == 0x7f800000u;
+    found |= bad;
+    if (bad) x[i] = 0;
+  }
+  return x;
+}
+
+// four consecutive activations
+__device__ __forceinline__ f32x4 load4(const bf16 *p) {
+  const uint2 x = *reinterpret_cast<const uint2 *>(p);
+  return f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
+               __uint_as_float(x.y & 0xffff0000u)};
+}
+__device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
+
+template <typename T, int D, int QT>
+__global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void verify_kernel(AttnVerifyArgs a, Split split, int qtiles) {
+  using L = Tile<T, D>;
+  constexpr int kKeyTiles = L::kKeys / 16;
+  constexpr int kRows = kWaves * QT * kQueries;
+  __shared__ __attribute__((aligned(16))) char stage[2][L::kBuffer];
+  __shared__ uint64_t anc_s[kWave];
+  __shared__ int bad_value;
+
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int g = lane / 16, col = lane % 16;
+  const int n = a.n, Hkv = a.cache.Hkv, G = a.Hq / Hkv, R = n * G;
+  unsigned u = blockIdx.x;
+  const int sp = u % split.n;
+  u /= split.n;
+  const int qt0 = u % qtiles * kRows;
+  u /= qtiles;
+  const int kv = u % Hkv, b = u / Hkv;
+  const int shift = a.cache.page_shift;
+
+  const int len = a.rows.len[b];
+  const int p = lane < n ? a.parent[(size_t)b * n + lane] : -1;
+  int err = SLA_OK;
+  if (!parents_ok(p, n, lane, a.chain)) err = SLA_ERR_TOPOLOGY;
+  else if (!length_ok(a.rows, shift, len, n) || len > a.max_len) err = SLA_ERR_LENGTH;
+  const int32_t *table = a.rows.table + (size_t)b * a.rows.max_pages;
+  const int total = err == SLA_OK ? len + n : 0;
+  if (a.status && kv == 0 && qt0 == 0 && sp == 0 && wave == 0) {
+    if (err == SLA_OK) {
+      bool bad = false;
+      for (int i = lane; i <= (total - 1) >> shift; i += kWave) bad |= (unsigned)table[i] >= (unsigned)a.cache.n_pages;
+      if (wave_any(bad)) err = SLA_ERR_PAGE;
+    }
+    if (lane == 0) a.status[b] = err;
+  }
+  if (err == SLA_ERR_TOPOLOGY || err == SLA_ERR_LENGTH) return;
+  const int k_begin = sp * split.chunk, k_end = min(k_begin + split.chunk, total);
+  if (k_begin >= k_end) return;
+
+  if (wave == 0) anc_s[lane] = node_ancestors(p, lane);
+  if (tid == 0) bad_value = 0;
+  __syncthreads();
+
+  // this wave's queries
+  const int r0 = qt0 + wave * QT * kQueries;
+  const bool active = r0 < R;
+  Frag<T, D> qf[QT];
+  uint64_t anc[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = min(r0 + t * kQueries + col, R - 1);
+    anc[t] = anc_s[r / G];
+    const T *q = static_cast<const T *>(a.q) + (((size_t)b * n + r / G) * a.Hq + (size_t)kv * G + r % G) * D;
+    if constexpr (L::kBf16) {
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) qf[t].x[c] = *reinterpret_cast<const bf16x8 *>(q + 32 * c + 8 * g);
+    } else {
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) qf[t].x[c] = *reinterpret_cast<const f32x4 *>(q + 16 * c + 4 * g);
+    }
+  }
+
+  f32x4 o[QT][D / 16];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float scale = a.scale * 1.44269504088896341f;  // weights are powers of two
+
+  // tile loads: this thread's row of each pass, and its page one tile ahead
+  const char *kbase = static_cast<const char *>(a.cache.k) + tid % L::kCols * 16;
+  const char *vbase = static_cast<const char *>(a.cache.v) + tid % L::kCols * 16;
+  const int prow = tid / L::kCols;
+  int page[L::kPasses];
+  u32x4 kreg[L::kPasses], vreg[L::kPasses];
+  // rows past the last one repeat it: they are masked
+  auto load_pages = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < L::kPasses; ++i) page[i] = table[min(k0 + i * L::kPassRows + prow, total - 1) >> shift];
+  };
+  auto load_rows = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < L::kPasses; ++i) {
+      const int k = min(k0 + i * L::kPassRows + prow, total - 1);
+      const int pg = (unsigned)page[i] < (unsigned)a.cache.n_pages ? page[i] : 0;
+      const size_t off = (page_row(a.cache, pg, kv) + (k & ((1 << shift) - 1))) * L::kRow;
+      kreg[i] = *reinterpret_cast<const u32x4 *>(kbase + off);
+      vreg[i] = *reinterpret_cast<const u32x4 *>(vbase + off);
+    }
+  };
+  load_pages(k_begin);
+  load_rows(k_begin);
+  load_pages(min(k_begin + L::kKeys, total - 1));
+
+  int buf = 0;
+  for (int k0 = k_begin; k0 < k_end; k0 += L::kKeys, buf ^= 1) {
+    char *const ks = stage[buf], *const vs = stage[buf] + L::kKeys * L::kPitchK;
+    const bool edge = k0 + L::kKeys > len;  // the tile reaches into the draft
+#pragma unroll
+    for (int i = 0; i < L::kPasses; ++i) {
+      const int row = i * L::kPassRows + prow;
+      // a weight of 0 does not remove an infinity or a NaN from a product: a
+      // draft row's are left out here and given to the queries that see the
+      // row at the end (a committed row's reach every query in any case)
+      if (edge && k0 + row >= len) {
+        bool found = false;
+        vreg[i] = finite_part(vreg[i], found, T{});
+        if (found) bad_value = 1;
+      }
+      *reinterpret_cast<u32x4 *>(ks + row * L::kPitchK + tid % L::kCols * 16) = kreg[i];
+      *reinterpret_cast<u32x4 *>(vs + row * L::kPitchV + tid % L::kCols * 16) = vreg[i];
+    }
+    if (k0 + L::kKeys < k_end) {
+      load_rows(k0 + L::kKeys);
+      load_pages(min(k0 + 2 * L::kKeys, total - 1));
+    }
+    __syncthreads();
+    if (!active) continue;
+
+    // scores, transposed: keys 4 g + i of key tile kt, query col
+    f32x4 s[QT][kKeyTiles];
+#pragma unroll
+    for (int kt = 0; kt < kKeyTiles; ++kt) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) s[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const char *row = ks + (kt * 16 + col) * L::kPitchK + g * 16;
+      if constexpr (L::kBf16) {
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(row + c * 64);
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+            s[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t].x[c], s[t][kt], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          const f32x4 kf = *reinterpret_cast<const f32x4 *>(row + c * 64);
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              s[t][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i], qf[t].x[c][i], s[t][kt], 0, 0, 0);
+        }
+      }
+    }
+    // running softmax
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float top = m[t];
+#pragma unroll
+      for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = s[t][kt][i] * scale;
+          if (edge) {
+            const int rel = k0 + kt * 16 + 4 * g + i - len;
+            if (rel >= 0 && !(rel < n && (anc[t] >> (rel & 63)) & 1ull)) x = -INFINITY;
+          }
+          s[t][kt][i] = x;
+          top = fmaxf(top, x);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float ref = top == -INFINITY ? 0.f : top;  // nothing visible yet: weights 0, not NaN
+      const float shrink = __builtin_amdgcn_exp2f(m[t] - ref);
+      m[t] = top;
+      float sum = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[t][kt][i] = __builtin_amdgcn_exp2f(s[t][kt][i] - ref);
+          sum += s[t][kt][i];
+        }
+      l[t] = l[t] * shrink + sum;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) o[t][d] *= shrink;
+    }
+
+    // O^T += V^T P^T
+    if constexpr (L::kBf16) {
+#pragma unroll
+      for (int kp = 0; kp < kKeyTiles / 2; ++kp) {
+        bf16x8 pf[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            pf[t][i] = static_cast<__bf16>(s[t][2 * kp][i]);
+            pf[t][4 + i] = static_cast<__bf16>(s[t][2 * kp + 1][i]);
+          }
+        // lane: row 4 g + col / 4 of a key tile, elements 4 (col % 4)..; it
+        // receives element col of rows 4 g..4 g + 3
+        char *row = vs + (kp * 32 + 4 * g + col / 4) * L::kPitchV + col % 4 * 8;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(row + d * 32));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(row + 16 * L::kPitchV + d * 32));
+          const bf16x8 vf = __builtin_bit_cast(
+              bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int t = 0; t < QT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], o[t][d], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float vf = reinterpret_cast<const float *>(vs + (kt * 16 + 4 * g + i) * L::kPitchV)[d * 16 + col];
+#pragma unroll
+            for (int t = 0; t < QT; ++t)
+              o[t][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, s[t][kt][i], o[t][d], 0, 0, 0);
+          }
+    }
+  }
+  if (!active) return;
+
+  if (bad_value) {  // written before the last tile's barrier
+    for (int k = max(k_begin, len); k < k_end; ++k) {
+      const int pg = table[k >> shift];
+      const T *row = static_cast<const T *>(a.cache.v) +
+                     (page_row(a.cache, (unsigned)pg < (unsigned)a.cache.n_pages ? pg : 0, kv) + (k & ((1 << shift) - 1))) * D;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) {
+        const f32x4 v = load4(row + d * 16 + 4 * g);
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!(fabsf(v[e]) < INFINITY) && (anc[t] >> (k - len)) & 1ull) o[t][d][e] += v[e];
+      }
+    }
+  }
+
+  const bool whole = split.chunk >= total;  // no other workgroup has keys of these rows
+  float *const ws = static_cast<float *>(a.workspace);
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    l[t] += __shfl_xor(l[t], 16);
+    l[t] += __shfl_xor(l[t], 32);
+    const int r = r0 + t * kQueries + col;
+    if (r >= R) continue;
+    if (whole) {
+      const float inv = 1.f / l[t];
+      T *out = static_cast<T *>(a.out) + (((size_t)b * n + r / G) * a.Hq + (size_t)kv * G + r % G) * D + 4 * g;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) {
+        const f32x4 x = o[t][d] * inv;
+        if constexpr (L::kBf16)
+          *reinterpret_cast<uint2 *>(out + d * 16) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+        else
+          *reinterpret_cast<f32x4 *>(out + d * 16) = x;
+      }
+    } else {
+      const size_t row = (((size_t)b * Hkv + kv) * split.n + sp) * R + r;
+      float *out = ws + row * D + 4 * g;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4 *>(out + d * 16) = o[t][d];
+      if (g == 0)
+        *reinterpret_cast<float2 *>(ws + (size_t)a.B * Hkv * split.n * R * D + row * 2) = make_float2(m[t], l[t]);
+    }
+  }
+}
+
+// Joins the splits of a row: D / 4 lanes hold it, four elements each.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split split) {
+  constexpr int kLanes = D / 4;
+  const int n = a.n, Hkv = a.cache.Hkv, G = a.Hq / Hkv, R = n * G;
+  const size_t rows = (size_t)a.B * Hkv * R;
+  const size_t i = (size_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
+  if (i >= rows) return;
+  const int r = i % R, kv = i / R % Hkv, b = i / R / Hkv;
+  const int len = a.rows.len[b];
+  if (!length_ok(a.rows, a.cache.page_shift, len, n) || len > a.max_len) return;
+  const int total = len + n;
+  if (split.chunk >= total) return;  // written whole
+  const int parts = (total + split.chunk - 1) / split.chunk;
+  const size_t first = ((size_t)b * Hkv + kv) * split.n * R + r;
+  const float *ws = static_cast<const float *>(a.workspace);
+  const float2 *ml = reinterpret_cast<const float2 *>(ws + rows * split.n * D);
+  const int e = threadIdx.x % kLanes * 4;
+  float top = -INFINITY;
+  for (int s = 0; s < parts; ++s) top = fmaxf(top, ml[first + (size_t)s * R].x);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float l = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < parts; ++s) {
+    const size_t row = first + (size_t)s * R;
+    const float2 st = ml[row];
+    const float w = __builtin_amdgcn_exp2f(st.x - ref);
+    l = __builtin_fmaf(w, st.y, l);
+    x += w * *reinterpret_cast<const f32x4 *>(ws + row * D + e);
+  }
+  x *= 1.f / l;
+  T *out = static_cast<T *>(a.out) + (((size_t)b * n + r / G) * a.Hq + (size_t)kv * G + r % G) * D + e;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2 *>(out) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+  else
+    *reinterpret_cast<f32x4 *>(out) = x;
+}
+
+// rows of a workgroup: 64, or 128 where there are more
+int query_tiles(int R) { return R > 64 ? 2 : 1; }
+
+Split plan(const AttnVerifyArgs &a, int keys) {
+  const int R = a.n * (a.Hq / a.cache.Hkv), rows = 64 * query_tiles(R);
+  const int64_t units = (int64_t)a.B * a.cache.Hkv * ((R + rows - 1) / rows);
+  const int64_t tiles = ((int64_t)a.max_len + a.n + keys - 1) / keys;
+  const int64_t want = (2 * device_cus() + units - 1) / units;
+  const int64_t per = (tiles + want - 1) / want;
+  return Split{(int)((tiles + per - 1) / per), (int)(per * keys)};
+}
+
+int tile_keys(int D, int dtype) { return 16384 / (D * (dtype == SLA_DTYPE_BF16 ? 2 : 4)); }
+
+template <typename T, int D>
+hipError_t launch_d(const AttnVerifyArgs &a, hipStream_t s) {
+  const int G = a.Hq / a.cache.Hkv, R = a.n * G, qt = query_tiles(R), qtiles = (R + 64 * qt - 1) / (64 * qt);
+  const Split split = plan(a, Tile<T, D>::kKeys);
+  const uint64_t blocks = (uint64_t)a.B * a.cache.Hkv * qtiles * split.n;
+  const uint64_t join = ((uint64_t)a.B * a.cache.Hkv * R + kThreads / (D / 4) - 1) / (kThreads / (D / 4));
+  if (blocks >= (1ull << 31) || join >= (1ull << 31)) return hipErrorInvalidValue;
+  if (qt == 1)
+    hipLaunchKernelGGL((verify_kernel<T, D, 1>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, split, qtiles);
+  else
+    hipLaunchKernelGGL((verify_kernel<T, D, 2>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, split, qtiles);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || split.n == 1) return e;
+  hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)join), dim3(kThreads), 0, s, a, split);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_t(const AttnVerifyArgs &a, hipStream_t s) {
+  switch (a.cache.D) {
+    case 64: return launch_d<T, 64>(a, s);
+    case 128: return launch_d<T, 128>(a, s);
+    default: return launch_d<T, 256>(a, s);
+  }
+}
+
+}  // namespace
+
+size_t attn_workspace_bytes(const AttnVerifyArgs &a, int dtype) {
+  const Split split = plan(a, tile_keys(a.cache.D, dtype));
+  if (split.n == 1) return 0;
+  return (size_t)a.B * a.Hq * a.n * split.n * (a.cache.D + 2) * sizeof(float);
+}
+
+hipError_t launch_attn_verify(const AttnVerifyArgs &a, int dtype, hipStream_t s) {
+  return dtype == SLA_DTYPE_BF16 ? launch_t<bf16>(a, s) : launch_t<float>(a, s);
+}
+
+}  // namespace sla

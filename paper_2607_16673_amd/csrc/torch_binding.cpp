@@ -67,6 +67,12 @@ long number(PyObject *o) {
   return v;
 }
 
+int32_t number32(PyObject *o, const char *name) {
+  const long v = number(o);
+  TORCH_CHECK_VALUE(v >= INT32_MIN && v <= INT32_MAX, name, " is out of range: ", v);
+  return (int32_t)v;
+}
+
 bool truth(PyObject *o) {
   const int v = PyObject_IsTrue(o);
   if (v < 0) throw python_error();
@@ -290,14 +296,222 @@ PyObject *prune(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// A layer's pool, or several layers': [layers][pages][kv heads][page size][D].
+struct Pool {
+  sla_attn_shape shape;
+  int32_t layers;
+  void *k, *v;
+  const at::Tensor *tensor;
+};
+
+Pool pool(PyObject *ko, PyObject *vo, bool layered) {
+  const at::Tensor &k = tensor(ko, "k_cache");
+  TORCH_CHECK_VALUE(k.dim() == 4 || (layered && k.dim() == 5), "k_cache must have ", layered ? "4 or 5" : "4",
+                    " dimensions, got ", k.dim());
+  const int64_t at0 = k.dim() - 4;
+  Pool p = {};
+  p.tensor = &k;
+  p.shape.qkv_dtype = activation_code(k);
+  for (int64_t i = 0; i < k.dim(); ++i)
+    TORCH_CHECK_VALUE(k.size(i) <= INT32_MAX, "k_cache has shape ", k.sizes(), ", too large");
+  p.layers = at0 ? (int32_t)k.size(0) : 1;
+  p.shape.n_pages = (int32_t)k.size(at0);
+  p.shape.kv_heads = (int32_t)k.size(at0 + 1);
+  p.shape.page_size = (int32_t)k.size(at0 + 2);
+  p.shape.head_dim = (int32_t)k.size(at0 + 3);
+  TORCH_CHECK_VALUE(k.is_cuda(), "k_cache must live on the GPU");
+  TORCH_CHECK_VALUE(k.is_contiguous(), "k_cache must be contiguous");
+  const at::Tensor &v = tensor(vo, "v_cache");
+  TORCH_CHECK_VALUE(v.is_cuda(), "v_cache must live on the GPU");
+  TORCH_CHECK_TYPE(v.scalar_type() == k.scalar_type(), "v_cache must be ", k.scalar_type(), ", got ", v.scalar_type());
+  TORCH_CHECK_VALUE(v.sizes() == k.sizes(), "v_cache has shape ", v.sizes(), ", expected ", k.sizes());
+  TORCH_CHECK_VALUE(v.is_contiguous(), "v_cache must be contiguous");
+  p.k = k.data_ptr();
+  p.v = v.data_ptr();
+  return p;
+}
+
+struct Rows {
+  const int32_t *parent, *table, *len;
+  int32_t *status;
+};
+
+// parent_idx [B][n], page_table [B][max_pages], cache_len [B], status [B] or None
+Rows cache_rows(sla_attn_shape &s, PyObject *parent, PyObject *table, PyObject *len, PyObject *status) {
+  const at::Tensor &p = sized(parent, 2, "parent_idx");
+  const at::Tensor &t = sized(table, 2, "page_table");
+  const int64_t B = p.size(0), n = p.size(1), pages = t.size(1);
+  s.batch = (int32_t)B;
+  s.n_nodes = (int32_t)n;
+  s.max_pages = (int32_t)pages;
+  Rows r;
+  r.parent = static_cast<const int32_t *>(device_pointer(p, at::kInt, {B, n}, "parent_idx"));
+  r.table = static_cast<const int32_t *>(device_pointer(t, at::kInt, {B, pages}, "page_table"));
+  r.len = static_cast<const int32_t *>(pointer(len, at::kInt, {B}, "cache_len"));
+  r.status = static_cast<int32_t *>(optional_pointer(status, at::kInt, {B}, "status"));
+  return r;
+}
+
+// a draft's projection [B][n][heads][D]: the heads of a node dense, the nodes a
+// constant step apart (a part of a wider projection)
+const void *strided(PyObject *o, at::ScalarType dtype, Dims shape, const char *name, int64_t &step) {
+  const at::Tensor &t = sized(o, 4, name);
+  TORCH_CHECK_VALUE(t.is_cuda(), name, " must live on the GPU");
+  TORCH_CHECK_TYPE(t.scalar_type() == dtype, name, " must be ", dtype, ", got ", t.scalar_type());
+  const at::IntArrayRef want(shape.begin(), shape.size());
+  TORCH_CHECK_VALUE(t.sizes() == want, name, " has shape ", t.sizes(), ", expected ", want);
+  const int64_t B = t.size(0), n = t.size(1), H = t.size(2), D = t.size(3);
+  step = n > 1 ? t.stride(1) : B > 1 ? t.stride(0) : H * D;
+  TORCH_CHECK_VALUE((D == 1 || t.stride(3) == 1) && (H == 1 || t.stride(2) == D) && (B == 1 || t.stride(0) == n * step) &&
+                        step >= H * D,
+                    name, " must hold each node's heads contiguously, its nodes a constant step apart; strides are ",
+                    t.strides());
+  return t.data_ptr();
+}
+
+// attn_append(q, k, v, parent_idx, page_table, cache_len, q_out, k_cache, v_cache, q_norm, k_norm, eps, rope, layout,
+//             status, topology)
+PyObject *attn_append(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  count_args(nargs, 16);
+  Pool c = pool(o[7], o[8], false);
+  const at::ScalarType act = c.tensor->scalar_type();
+  const Rows r = cache_rows(c.shape, o[3], o[4], o[5], o[14]);
+  const int64_t B = c.shape.batch, n = c.shape.n_nodes, D = c.shape.head_dim, kh = c.shape.kv_heads;
+  const at::Tensor &q = sized(o[0], 4, "q");
+  const int64_t qh = q.size(2);
+  c.shape.q_heads = (int32_t)qh;
+  c.shape.topology = (int32_t)number(o[15]);
+  int64_t qs, ks, vs;
+  const void *qp = strided(o[0], act, {B, n, qh, D}, "q", qs);
+  const void *kp = strided(o[1], act, {B, n, kh, D}, "k", ks);
+  const void *vp = strided(o[2], act, {B, n, kh, D}, "v", vs);
+  void *out = pointer(o[6], act, {B, n, qh, D}, "q_out");
+  sla_attn_transform t = {};
+  t.q_norm = static_cast<const float *>(optional_pointer(o[9], at::kFloat, {D}, "q_norm"));
+  t.k_norm = static_cast<const float *>(optional_pointer(o[10], at::kFloat, {D}, "k_norm"));
+  const double eps = PyFloat_AsDouble(o[11]);
+  if (eps == -1.0 && PyErr_Occurred()) throw python_error();
+  t.eps = (float)eps;
+  if (o[12] != Py_None) {
+    const at::Tensor &rope = sized(o[12], 2, "rope");
+    t.rope = static_cast<const float *>(device_pointer(rope, at::kFloat, {rope.size(0), rope.size(1)}, "rope"));
+    TORCH_CHECK_VALUE(rope.size(0) <= INT32_MAX && rope.size(1) <= D, "rope has shape ", rope.sizes(), ", expected [positions][up to ", D, "]");
+    t.rope_len = (int32_t)rope.size(0);
+    t.rope_dim = (int32_t)rope.size(1);
+  }
+  t.layout = (int32_t)number(o[13]);
+  const hipStream_t stream = stream_of(*c.tensor);
+  return PyLong_FromLong(unlocked([&] {
+    return sla_attn_append(&c.shape, &t, qp, qs, kp, ks, vp, vs, r.parent, r.table, r.len, out, c.k, c.v, r.status,
+        stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+// q [B][n][q heads][D] of a verification over this pool
+const void *queries(Pool &c, PyObject *qo, PyObject *max_len) {
+  const at::Tensor &q = sized(qo, 4, "q");
+  c.shape.q_heads = (int32_t)q.size(2);
+  c.shape.max_len = number32(max_len, "max_len");
+  const int64_t B = c.shape.batch, n = c.shape.n_nodes, D = c.shape.head_dim;
+  return device_pointer(q, c.tensor->scalar_type(), {B, n, q.size(2), D}, "q");
+}
+
+// attn_verify(q, k_cache, v_cache, parent_idx, page_table, cache_len, out, scale, max_len, workspace, status, topology)
+PyObject *attn_verify(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  count_args(nargs, 12);
+  Pool c = pool(o[1], o[2], false);
+  const Rows r = cache_rows(c.shape, o[3], o[4], o[5], o[10]);
+  const void *q = queries(c, o[0], o[8]);
+  c.shape.topology = (int32_t)number(o[11]);
+  const int64_t B = c.shape.batch, n = c.shape.n_nodes, D = c.shape.head_dim;
+  void *out = pointer(o[6], c.tensor->scalar_type(), {B, n, (int64_t)c.shape.q_heads, D}, "out");
+  const double scale = PyFloat_AsDouble(o[7]);
+  if (scale == -1.0 && PyErr_Occurred()) throw python_error();
+  void *ws = nullptr;
+  size_t bytes = 0;
+  if (o[9] != Py_None) {
+    const at::Tensor &w = sized(o[9], 1, "workspace");
+    ws = device_pointer(w, at::kByte, {w.size(0)}, "workspace");
+    bytes = (size_t)w.size(0);
+  }
+  const hipStream_t stream = stream_of(*c.tensor);
+  return PyLong_FromLong(unlocked([&] {
+    return sla_attn_verify(&c.shape, (float)scale, q, c.k, c.v, r.parent, r.table, r.len, out, ws, bytes, r.status, stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+// attn_workspace_bytes(batch, n, q_heads, k_cache, max_pages, max_len)
+PyObject *attn_workspace_bytes(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  count_args(nargs, 6);
+  Pool c = pool(o[3], o[3], false);
+  c.shape.batch = (int32_t)number(o[0]);
+  c.shape.n_nodes = (int32_t)number(o[1]);
+  c.shape.q_heads = (int32_t)number(o[2]);
+  c.shape.max_pages = (int32_t)number(o[4]);
+  c.shape.max_len = number32(o[5], "max_len");
+  return PyLong_FromSize_t(sla_attn_workspace_bytes(&c.shape));
+  END_HANDLE_TH_ERRORS
+}
+
+// attn_commit(k_cache, v_cache, parent_idx, path, len, page_table, cache_len, new_len | None, status)
+PyObject *attn_commit(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  count_args(nargs, 9);
+  Pool c = pool(o[0], o[1], true);
+  const Rows r = cache_rows(c.shape, o[2], o[5], o[6], o[8]);
+  const int64_t B = c.shape.batch, n = c.shape.n_nodes;
+  const void *path = pointer(o[3], at::kInt, {B, n}, "path");
+  const void *len = pointer(o[4], at::kInt, {B}, "len");
+  void *new_len = optional_pointer(o[7], at::kInt, {B}, "new_len");
+  const hipStream_t stream = stream_of(*c.tensor);
+  return PyLong_FromLong(unlocked([&] {
+    return sla_attn_commit(&c.shape, c.layers, c.k, c.v, r.parent, static_cast<const int32_t *>(path),
+        static_cast<const int32_t *>(len), r.table, r.len, static_cast<int32_t *>(new_len), r.status, stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+// page_copy(k_cache, v_cache, src, dst, rows | None, status | None)
+PyObject *page_copy(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  count_args(nargs, 6);
+  Pool c = pool(o[0], o[1], true);
+  const at::Tensor &src = sized(o[2], 1, "src");
+  const int64_t m = src.size(0);
+  TORCH_CHECK_VALUE(m <= INT32_MAX, "src has shape ", src.sizes(), ", too large");
+  const void *sp = device_pointer(src, at::kInt, {m}, "src");
+  const void *dp = pointer(o[3], at::kInt, {m}, "dst");
+  const void *rp = optional_pointer(o[4], at::kInt, {m}, "rows");
+  void *status = optional_pointer(o[5], at::kInt, {m}, "status");
+  const hipStream_t stream = stream_of(*c.tensor);
+  return PyLong_FromLong(unlocked([&] {
+    return sla_page_copy(&c.shape, c.layers, c.k, c.v, static_cast<const int32_t *>(sp), static_cast<const int32_t *>(dp),
+        static_cast<const int32_t *>(rp), (int32_t)m, static_cast<int32_t *>(status), stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)>
 constexpr PyMethodDef method(const char *name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
 }
 
-PyMethodDef methods[] = {method<verify>("verify"),           method<commit>("commit"),
-    method<conv_verify>("conv_verify"),
-                         method<conv_commit>("conv_commit"), method<prune>("prune"),   {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {method<verify>("verify"),
+                         method<commit>("commit"),
+                         method<conv_verify>("conv_verify"),
+                         method<conv_commit>("conv_commit"),
+                         method<prune>("prune"),
+                         method<attn_append>("attn_append"),
+                         method<attn_verify>("attn_verify"),
+                         method<attn_workspace_bytes>("attn_workspace_bytes"),
+                         method<attn_commit>("attn_commit"),
+                         method<page_copy>("page_copy"),
+                         {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of libsla's device calls.", -1, methods};
 
