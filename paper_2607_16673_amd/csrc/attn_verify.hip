@@ -28,6 +28,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kQueries = 16;  // queries of one matrix tile
+constexpr float kSlack = 8.f;      // how far, in powers of two, a score may pass its softmax's reference
+constexpr float kNoScore = -3e38f;  // the reference before the first visible key
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -150,10 +152,17 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
     const T *q = static_cast<const T *>(a.q) + (((size_t)b * n + r / G) * a.Hq + (size_t)kv * G + r % G) * D;
     if constexpr (L::kBf16) {
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) qf[t].x[c] = *reinterpret_cast<const bf16x8 *>(q + 32 * c + 8 * g);
+      for (int c = 0; c < D / 32; ++c) {
+        u32x4 x = *reinterpret_cast<const u32x4 *>(q + 32 * c + 8 * g);
+        if (a.scale < 0.f) x ^= 0x80008000u;
+        qf[t].x[c] = __builtin_bit_cast(bf16x8, x);
+      }
     } else {
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) qf[t].x[c] = *reinterpret_cast<const f32x4 *>(q + 16 * c + 4 * g);
+      for (int c = 0; c < D / 16; ++c) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(q + 16 * c + 4 * g);
+        qf[t].x[c] = a.scale < 0.f ? -x : x;
+      }
     }
   }
 
@@ -161,12 +170,14 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
   float m[QT], l[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    m[t] = -INFINITY;
+    m[t] = kNoScore;
     l[t] = 0.f;
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const float scale = a.scale * 1.44269504088896341f;  // weights are powers of two
+  // weights are powers of two; the scale's sign is in the queries, and a scale
+  // of 0 is one too small to part any scores, so that masked ones stay -inf
+  const float scale = fmaxf(fabsf(a.scale) * 1.44269504088896341f, 1e-30f);
 
   // tile loads: this thread's row of each pass, and its page one tile ahead
   const char *kbase = static_cast<const char *>(a.cache.k) + tid % L::kCols * 16;
@@ -245,38 +256,48 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
         }
       }
     }
-    // running softmax
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float top = m[t];
+    // softmax against a reference that only moves when a score exceeds it by
+    // more than 2^kSlack: weights stay below 2^kSlack, where fp32 sums and bf16
+    // weights are as precise as below 1, and most tiles neither reduce a
+    // maximum over the lanes nor rescale the output
+    if (edge) {
 #pragma unroll
       for (int kt = 0; kt < kKeyTiles; ++kt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float x = s[t][kt][i] * scale;
-          if (edge) {
-            const int rel = k0 + kt * 16 + 4 * g + i - len;
-            if (rel >= 0 && !(rel < n && (anc[t] >> (rel & 63)) & 1ull)) x = -INFINITY;
-          }
-          s[t][kt][i] = x;
-          top = fmaxf(top, x);
+          const int rel = k0 + kt * 16 + 4 * g + i - len;
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+            if (rel >= 0 && !(rel < n && (anc[t] >> (rel & 63)) & 1ull)) s[t][kt][i] = -INFINITY;
         }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float ref = top == -INFINITY ? 0.f : top;  // nothing visible yet: weights 0, not NaN
-      const float shrink = __builtin_amdgcn_exp2f(m[t] - ref);
-      m[t] = top;
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][kt][i]);
+      top *= scale;
+      if (wave_any(top - m[t] > kSlack)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        top = fmaxf(top, m[t]);
+        const float shrink = __builtin_amdgcn_exp2f(m[t] - top);
+        m[t] = top;
+        l[t] *= shrink;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[t][d] *= shrink;
+      }
       float sum = 0.f;
 #pragma unroll
       for (int kt = 0; kt < kKeyTiles; ++kt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          s[t][kt][i] = __builtin_amdgcn_exp2f(s[t][kt][i] - ref);
+          s[t][kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][kt][i], scale, -m[t]));
           sum += s[t][kt][i];
         }
-      l[t] = l[t] * shrink + sum;
-#pragma unroll
-      for (int d = 0; d < D / 16; ++d) o[t][d] *= shrink;
+      l[t] += sum;
     }
 
     // O^T += V^T P^T
@@ -385,9 +406,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
   const float *ws = static_cast<const float *>(a.workspace);
   const float2 *ml = reinterpret_cast<const float2 *>(ws + rows * split.n * D);
   const int e = threadIdx.x % kLanes * 4;
-  float top = -INFINITY;
-  for (int s = 0; s < parts; ++s) top = fmaxf(top, ml[first + (size_t)s * R].x);
-  const float ref = top == -INFINITY ? 0.f : top;
+  float ref = kNoScore;
+  for (int s = 0; s < parts; ++s) ref = fmaxf(ref, ml[first + (size_t)s * R].x);
   float l = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   for (int s = 0; s < parts; ++s) {
