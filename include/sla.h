@@ -413,7 +413,7 @@ typedef struct sla_attn_shape {
   int32_t page_size; /* rows of a page: 16, 32, 64, 128 or 256              */
   int32_t n_pages;   /* pages of the pool                                   */
   int32_t max_pages; /* entries of a page-table row; max_pages page_size
-                        < 2^31                                              */
+                        <= 2^30                                             */
   int32_t max_len;   /* promise that cache_len[b] <= max_len, by which
                         sla_attn_verify lays out its work; 0: none, the
                         page table's capacity                               */

@@ -41,7 +41,7 @@ int check_rows(const sla_attn_shape *s) {
   if (st != SLA_OK) return st;
   if (s->batch < 1 || s->batch > 65535 || s->n_nodes < 1 || s->n_nodes > SLA_MAX_NODES || s->max_pages < 1)
     return SLA_ERR_SHAPE;
-  if ((int64_t)s->max_pages * s->page_size >= (1ll << 31)) return SLA_ERR_SHAPE;
+  if ((int64_t)s->max_pages * s->page_size > (1ll << 30)) return SLA_ERR_SHAPE;
   return SLA_OK;
 }
 

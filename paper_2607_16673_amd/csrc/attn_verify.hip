@@ -25,8 +25,8 @@
 namespace sla {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
+constexpr int kThreads = 256;  // of the join kernel
+constexpr int kMaxWaves = 8;   // of the attention kernel
 constexpr int kQueries = 16;  // queries of one matrix tile
 constexpr float kSlack = 8.f;      // how far, in powers of two, a score may pass its softmax's reference
 constexpr float kNoScore = -3e38f;  // the reference before the first visible key
@@ -37,19 +37,25 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
+// A tile of keys and values in LDS, 16 KB each, filled by direct loads: 64
+// lanes bring 1 KB, one 16-byte piece a lane, to consecutive addresses.  Piece
+// c of row r lies at piece c ^ swizzle(r) of its row, so that a wave's fragment
+// reads spread over the banks: 16 rows of one piece for K; for V four rows of
+// two (bf16) or four (fp32) neighbouring ones.
 template <typename T, int D>
 struct Tile {
   static constexpr bool kBf16 = sizeof(T) == 2;
   static constexpr int kRow = D * (int)sizeof(T);  // bytes of a row
-  static constexpr int kKeys = 16384 / kRow;       // rows of a tile
-  // rows are padded so that a wave's fragment reads spread over the banks: 16
-  // rows a 16-byte step apart for K; for V four rows of 32 bytes each in bf16
-  static constexpr int kPitchK = kRow + 16;
-  static constexpr int kPitchV = kRow + (kBf16 ? 32 : 16);
-  static constexpr int kCols = kRow / 16;                // 16-byte pieces of a row
-  static constexpr int kPassRows = kThreads / kCols;     // rows one pass of the workgroup loads
-  static constexpr int kPasses = kKeys / kPassRows;
-  static constexpr int kBuffer = kKeys * (kPitchK + kPitchV);
+  static constexpr int kBytes = 16384;
+  static constexpr int kKeys = kBytes / kRow;
+  static constexpr int kCols = kRow / 16;      // pieces of a row
+  static constexpr int kLoads = kBytes / 1024;  // direct loads that fill the tile
+  static constexpr int kLoadRows = 1024 / kRow; // rows of one of them, 1..8
+  static_assert(kLoadRows >= 1 && kLoadRows <= 8, "a direct load stays in one page");
+  __host__ __device__ static constexpr int swizzle_k(int r) { return kRow >= 256 ? r % 16 : r / 2 % 8; }
+  __host__ __device__ static constexpr int swizzle_v(int r) {
+    return !kBf16 ? r & 12 : kRow >= 256 ? r * 2 % 16 : r & 6;
+  }
 };
 
 struct Split {
@@ -97,22 +103,25 @@ __device__ __forceinline__ f32x4 load4(const bf16 *p) {
 }
 __device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
 
-template <typename T, int D, int QT>
-__global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void verify_kernel(AttnVerifyArgs a, Split split, int qtiles) {
+// WK waves share a query's keys (each takes its part of every tile), the
+// workgroup's waves / WK groups of them take QT query tiles each.
+template <typename T, int D, int QT, int WK>
+__global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArgs a, Split split, int qtiles) {
   using L = Tile<T, D>;
-  constexpr int kKeyTiles = L::kKeys / 16;
-  constexpr int kRows = kWaves * QT * kQueries;
-  __shared__ __attribute__((aligned(16))) char stage[2][L::kBuffer];
+  constexpr int kKeyTiles = L::kKeys / 16 / WK;  // of a wave
+  static_assert(kKeyTiles >= 1 && (!L::kBf16 || kKeyTiles == 1 || kKeyTiles % 2 == 0), "whole matrix tiles");
+  __shared__ __attribute__((aligned(1024))) char stage[2][2 * L::kBytes];
   __shared__ uint64_t anc_s[kWave];
   __shared__ int bad_value;
 
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int tid = threadIdx.x, lane = tid % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), waves = blockDim.x / kWave;
   const int g = lane / 16, col = lane % 16;
   const int n = a.n, Hkv = a.cache.Hkv, G = a.Hq / Hkv, R = n * G;
   unsigned u = blockIdx.x;
   const int sp = u % split.n;
   u /= split.n;
-  const int qt0 = u % qtiles * kRows;
+  const int qt0 = u % qtiles * (waves / WK * QT * kQueries);
   u /= qtiles;
   const int kv = u % Hkv, b = u / Hkv;
   const int shift = a.cache.page_shift;
@@ -138,10 +147,34 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
 
   if (wave == 0) anc_s[lane] = node_ancestors(p, lane);
   if (tid == 0) bad_value = 0;
-  __syncthreads();
 
-  // this wave's queries
-  const int r0 = qt0 + wave * QT * kQueries;
+  // tile loads.  Lane i < 16 holds the page of the tile's rows 16 i..16 i + 15;
+  // rows past the last one come from wherever the last page's row would be, and
+  // are masked
+  const char *const kbase = static_cast<const char *>(a.cache.k), *const vbase = static_cast<const char *>(a.cache.v);
+  const int last = (total - 1) >> shift;
+  auto load_pages = [&](int k0) {
+    return table[min((k0 + lane % 16 * 16) >> shift, last)];
+  };
+  const int load_row = lane / L::kCols, load_col = lane % L::kCols;
+  auto load_tile = [&](int k0, int pages, char *dst) {
+    pages = (unsigned)pages < (unsigned)a.cache.n_pages ? pages : 0;
+    for (int c = wave; c < L::kLoads; c += waves) {
+      const int first = c * L::kLoadRows;  // the load's first row in the tile
+      const int pg = __builtin_amdgcn_readlane(pages, first / 16);
+      const size_t off = (page_row(a.cache, pg, kv) + ((k0 + first) & ((1 << shift) - 1))) * L::kRow;
+      const int r = first + load_row;
+      load_lds16(kbase + off + load_row * L::kRow + ((load_col ^ L::swizzle_k(r)) * 16), dst + c * 1024);
+      load_lds16(vbase + off + load_row * L::kRow + ((load_col ^ L::swizzle_v(r)) * 16), dst + L::kBytes + c * 1024);
+    }
+  };
+  int pages = load_pages(k_begin);
+  load_tile(k_begin, pages, stage[0]);
+  pages = load_pages(k_begin + L::kKeys);
+
+  // this wave's queries, and their ancestors
+  __syncthreads();
+  const int r0 = qt0 + wave / WK * (QT * kQueries), wk = wave % WK;
   const bool active = r0 < R;
   Frag<T, D> qf[QT];
   uint64_t anc[QT];
@@ -179,55 +212,42 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
   // of 0 is one too small to part any scores, so that masked ones stay -inf
   const float scale = fmaxf(fabsf(a.scale) * 1.44269504088896341f, 1e-30f);
 
-  // tile loads: this thread's row of each pass, and its page one tile ahead
-  const char *kbase = static_cast<const char *>(a.cache.k) + tid % L::kCols * 16;
-  const char *vbase = static_cast<const char *>(a.cache.v) + tid % L::kCols * 16;
-  const int prow = tid / L::kCols;
-  int page[L::kPasses];
-  u32x4 kreg[L::kPasses], vreg[L::kPasses];
-  // rows past the last one repeat it: they are masked
-  auto load_pages = [&](int k0) {
-#pragma unroll
-    for (int i = 0; i < L::kPasses; ++i) page[i] = table[min(k0 + i * L::kPassRows + prow, total - 1) >> shift];
-  };
-  auto load_rows = [&](int k0) {
-#pragma unroll
-    for (int i = 0; i < L::kPasses; ++i) {
-      const int k = min(k0 + i * L::kPassRows + prow, total - 1);
-      const int pg = (unsigned)page[i] < (unsigned)a.cache.n_pages ? page[i] : 0;
-      const size_t off = (page_row(a.cache, pg, kv) + (k & ((1 << shift) - 1))) * L::kRow;
-      kreg[i] = *reinterpret_cast<const u32x4 *>(kbase + off);
-      vreg[i] = *reinterpret_cast<const u32x4 *>(vbase + off);
-    }
-  };
-  load_pages(k_begin);
-  load_rows(k_begin);
-  load_pages(min(k_begin + L::kKeys, total - 1));
+  // fragment reads: this lane's row of a key tile, and the pieces' places in it
+  const int k_row = (wk * kKeyTiles * 16 + col) * L::kRow;
+  const int k_piece = (g ^ L::swizzle_k(col)) * 16;
+  // V, bf16: row 4 g + col / 4 of a key tile, 8 bytes of the piece pair of 16
+  // elements; the lane receives element col of rows 4 g..4 g + 3.  fp32: row
+  // 4 g + i, element col.
+  const int v_in = L::kBf16 ? 4 * g + col / 4 : 4 * g;
+  const int v_row = L::kBytes + (wk * kKeyTiles * 16 + v_in) * L::kRow;
+  const int v_piece = L::kBf16 ? ((col % 4 / 2) ^ L::swizzle_v(v_in)) * 16 + col % 2 * 8
+                               : ((col / 4) ^ L::swizzle_v(v_in)) * 16 + col % 4 * 4;
 
-  int buf = 0;
-  for (int k0 = k_begin; k0 < k_end; k0 += L::kKeys, buf ^= 1) {
-    char *const ks = stage[buf], *const vs = stage[buf] + L::kKeys * L::kPitchK;
+  // attends to the staged tile `cur` while the next one's loads run
+  auto step = [&](int k0, char *__restrict__ cur, char *__restrict__ next) {
+    if (k0 + L::kKeys < k_end) {
+      load_tile(k0 + L::kKeys, pages, next);
+      pages = load_pages(k0 + 2 * L::kKeys);
+    }
     const bool edge = k0 + L::kKeys > len;  // the tile reaches into the draft
-#pragma unroll
-    for (int i = 0; i < L::kPasses; ++i) {
-      const int row = i * L::kPassRows + prow;
+    if (edge) {
       // a weight of 0 does not remove an infinity or a NaN from a product: a
       // draft row's are left out here and given to the queries that see the
       // row at the end (a committed row's reach every query in any case)
-      if (edge && k0 + row >= len) {
+      for (int c = tid; c < L::kBytes / 16; c += blockDim.x) {
+        const int k = k0 + c / L::kCols;
+        if (k < len) continue;
+        u32x4 *const piece = reinterpret_cast<u32x4 *>(cur + L::kBytes) + c;
         bool found = false;
-        vreg[i] = finite_part(vreg[i], found, T{});
-        if (found) bad_value = 1;
+        const u32x4 x = finite_part(*piece, found, T{});
+        if (found) {
+          *piece = x;
+          if (k < total) bad_value = 1;
+        }
       }
-      *reinterpret_cast<u32x4 *>(ks + row * L::kPitchK + tid % L::kCols * 16) = kreg[i];
-      *reinterpret_cast<u32x4 *>(vs + row * L::kPitchV + tid % L::kCols * 16) = vreg[i];
+      __syncthreads();
     }
-    if (k0 + L::kKeys < k_end) {
-      load_rows(k0 + L::kKeys);
-      load_pages(min(k0 + 2 * L::kKeys, total - 1));
-    }
-    __syncthreads();
-    if (!active) continue;
+    if (!active) return;
 
     // scores, transposed: keys 4 g + i of key tile kt, query col
     f32x4 s[QT][kKeyTiles];
@@ -235,11 +255,11 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
     for (int kt = 0; kt < kKeyTiles; ++kt) {
 #pragma unroll
       for (int t = 0; t < QT; ++t) s[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const char *row = ks + (kt * 16 + col) * L::kPitchK + g * 16;
+      const char *row = cur + k_row + kt * 16 * L::kRow;
       if constexpr (L::kBf16) {
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(row + c * 64);
+          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(row + (c * 64 ^ k_piece));
 #pragma unroll
           for (int t = 0; t < QT; ++t)
             s[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t].x[c], s[t][kt], 0, 0, 0);
@@ -247,7 +267,7 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
       } else {
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-          const f32x4 kf = *reinterpret_cast<const f32x4 *>(row + c * 64);
+          const f32x4 kf = *reinterpret_cast<const f32x4 *>(row + (c * 64 ^ k_piece));
 #pragma unroll
           for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -256,21 +276,26 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
         }
       }
     }
+    if (edge) {
+#pragma unroll
+      for (int kt = 0; kt < kKeyTiles; ++kt) {
+        // bit i: the query sees key 4 g + i, draft node rel + i.  Bits of nodes
+        // past the draft are clear in every mask.
+        const int rel = k0 + (wk * kKeyTiles + kt) * 16 + 4 * g - len;
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          const int up = -rel & 63;
+          uint64_t see = rel >= 0 ? anc[t] >> (rel & 63) : anc[t] << up | ((1ull << up) - 1);
+          see = rel >= 64 ? 0 : rel <= -4 ? ~0ull : see;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][kt][i] = (uint32_t)see >> i & 1 ? s[t][kt][i] : -INFINITY;
+        }
+      }
+    }
     // softmax against a reference that only moves when a score exceeds it by
     // more than 2^kSlack: weights stay below 2^kSlack, where fp32 sums and bf16
     // weights are as precise as below 1, and most tiles neither reduce a
     // maximum over the lanes nor rescale the output
-    if (edge) {
-#pragma unroll
-      for (int kt = 0; kt < kKeyTiles; ++kt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int rel = k0 + kt * 16 + 4 * g + i - len;
-#pragma unroll
-          for (int t = 0; t < QT; ++t)
-            if (rel >= 0 && !(rel < n && (anc[t] >> (rel & 63)) & 1ull)) s[t][kt][i] = -INFINITY;
-        }
-    }
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       float top = -INFINITY;
@@ -301,7 +326,7 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
     }
 
     // O^T += V^T P^T
-    if constexpr (L::kBf16) {
+    if constexpr (L::kBf16 && kKeyTiles > 1) {
 #pragma unroll
       for (int kp = 0; kp < kKeyTiles / 2; ++kp) {
         bf16x8 pf[QT];
@@ -312,18 +337,28 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
             pf[t][i] = static_cast<__bf16>(s[t][2 * kp][i]);
             pf[t][4 + i] = static_cast<__bf16>(s[t][2 * kp + 1][i]);
           }
-        // lane: row 4 g + col / 4 of a key tile, elements 4 (col % 4)..; it
-        // receives element col of rows 4 g..4 g + 3
-        char *row = vs + (kp * 32 + 4 * g + col / 4) * L::kPitchV + col % 4 * 8;
+        char *row = cur + v_row + kp * 32 * L::kRow;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(row + d * 32));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(row + 16 * L::kPitchV + d * 32));
-          const bf16x8 vf = __builtin_bit_cast(
-              bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+          char *piece = row + (d * 32 ^ v_piece);
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)piece);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(piece + 16 * L::kRow));
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
           for (int t = 0; t < QT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], o[t][d], 0, 0, 0);
         }
+      }
+    } else if constexpr (L::kBf16) {
+      s16x4 pf[QT];
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pf[t][i] = __builtin_bit_cast(short, static_cast<__bf16>(s[t][0][i]));
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) {
+        const s16x4 vf = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(cur + v_row + (d * 32 ^ v_piece)));
+#pragma unroll
+        for (int t = 0; t < QT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, pf[t], o[t][d], 0, 0, 0);
       }
     } else {
 #pragma unroll
@@ -332,12 +367,65 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
         for (int d = 0; d < D / 16; ++d)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float vf = reinterpret_cast<const float *>(vs + (kt * 16 + 4 * g + i) * L::kPitchV)[d * 16 + col];
+            const float vf = *reinterpret_cast<const float *>(cur + v_row + (kt * 16 + i) * L::kRow + (d * 64 ^ v_piece));
 #pragma unroll
             for (int t = 0; t < QT; ++t)
               o[t][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, s[t][kt][i], o[t][d], 0, 0, 0);
           }
     }
+  };
+
+  int buf = 0;
+  for (int k0 = k_begin; k0 < k_end; k0 += L::kKeys, buf ^= 1) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the tile has landed
+    __syncthreads();                     // and every other wave's; the other buffer is free
+    step(k0, stage[buf], stage[buf ^ 1]);
+  }
+
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    l[t] += __shfl_xor(l[t], 16);
+    l[t] += __shfl_xor(l[t], 32);
+  }
+  if constexpr (WK > 1) {
+    // the waves of a query join theirs, half of them handing over to the rest
+    // in each round
+    float *const box = reinterpret_cast<float *>(stage[0]);
+    constexpr int kBox = QT * (D / 16 * 4 + 2) * kWave;  // floats of a wave
+    static_assert(WK / 2 * kBox * 4 <= (int)sizeof(stage), "the first round's hand-over fits");
+#pragma unroll
+    for (int half = WK / 2; half >= 1; half /= 2) {
+      __syncthreads();
+      float *const own = box + (wk % half) * kBox + lane;
+      if (wk >= half && wk < 2 * half) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          float *x = own + t * (D / 16 * 4 + 2) * kWave;
+          x[0] = m[t];
+          x[kWave] = l[t];
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[(2 + d * 4 + i) * kWave] = o[t][d][i];
+        }
+      }
+      __syncthreads();
+      if (wk < half) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          const float *x = own + t * (D / 16 * 4 + 2) * kWave;
+          const float top = fmaxf(m[t], x[0]);
+          const float w0 = __builtin_amdgcn_exp2f(m[t] - top), w1 = __builtin_amdgcn_exp2f(x[0] - top);
+          m[t] = top;
+          l[t] = w0 * l[t] + w1 * x[kWave];
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[t][d][i] = w0 * o[t][d][i] + w1 * x[(2 + d * 4 + i) * kWave];
+        }
+      }
+    }
+    if (wk > 0) return;
   }
   if (!active) return;
 
@@ -362,8 +450,6 @@ __global__ __launch_bounds__(kThreads, QT * D * sizeof(T) >= 1024 ? 1 : 2) void 
   float *const ws = static_cast<float *>(a.workspace);
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    l[t] += __shfl_xor(l[t], 16);
-    l[t] += __shfl_xor(l[t], 32);
     const int r = r0 + t * kQueries + col;
     if (r >= R) continue;
     if (whole) {
@@ -425,33 +511,60 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
     *reinterpret_cast<f32x4 *>(out) = x;
 }
 
-// rows of a workgroup: 64, or 128 where there are more
-int query_tiles(int R) { return R > 64 ? 2 : 1; }
+// How a workgroup is laid out for R rows of a kv head.
+struct Form {
+  int qt, wk, waves;
+  int rows() const { return waves / wk * qt * kQueries; }
+};
 
-Split plan(const AttnVerifyArgs &a, int keys) {
-  const int R = a.n * (a.Hq / a.cache.Hkv), rows = 64 * query_tiles(R);
-  const int64_t units = (int64_t)a.B * a.cache.Hkv * ((R + rows - 1) / rows);
-  const int64_t tiles = ((int64_t)a.max_len + a.n + keys - 1) / keys;
-  const int64_t want = (2 * device_cus() + units - 1) / units;
-  const int64_t per = (tiles + want - 1) / want;
-  return Split{(int)((tiles + per - 1) / per), (int)(per * keys)};
+Form form_of(int R, int dtype) {
+  const int tiles = (R + kQueries - 1) / kQueries;
+  if (tiles == 1) return Form{1, 4, 4};
+  if (dtype == SLA_DTYPE_F32 || tiles <= 4) return Form{1, 1, tiles < kMaxWaves ? tiles : kMaxWaves};
+  return Form{2, 1, (tiles + 1) / 2 < kMaxWaves ? (tiles + 1) / 2 : kMaxWaves};
 }
 
 int tile_keys(int D, int dtype) { return 16384 / (D * (dtype == SLA_DTYPE_BF16 ? 2 : 4)); }
 
+Split plan(const AttnVerifyArgs &a, int dtype) {
+  const int R = a.n * (a.Hq / a.cache.Hkv), keys = tile_keys(a.cache.D, dtype);
+  const Form f = form_of(R, dtype);
+  const int64_t units = (int64_t)a.B * a.cache.Hkv * ((R + f.rows() - 1) / f.rows());
+  const int64_t tiles = ((int64_t)a.max_len + a.n + keys - 1) / keys;
+  const int64_t want = ((f.waves > 4 ? 1 : 2) * device_cus() + units - 1) / units;
+  const int64_t per = (tiles + want - 1) / want;
+  return Split{(int)((tiles + per - 1) / per), (int)(per * keys)};
+}
+
+template <typename T, int D, int QT, int WK>
+hipError_t launch_form(const AttnVerifyArgs &a, const Form &f, const Split &split, hipStream_t s) {
+  const int R = a.n * (a.Hq / a.cache.Hkv), qtiles = (R + f.rows() - 1) / f.rows();
+  const uint64_t blocks = (uint64_t)a.B * a.cache.Hkv * qtiles * split.n;
+  if (blocks >= (1ull << 31)) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((verify_kernel<T, D, QT, WK>), dim3((unsigned)blocks), dim3((unsigned)f.waves * kWave), 0, s, a, split,
+                     qtiles);
+  return hipGetLastError();
+}
+
 template <typename T, int D>
 hipError_t launch_d(const AttnVerifyArgs &a, hipStream_t s) {
-  const int G = a.Hq / a.cache.Hkv, R = a.n * G, qt = query_tiles(R), qtiles = (R + 64 * qt - 1) / (64 * qt);
-  const Split split = plan(a, Tile<T, D>::kKeys);
-  const uint64_t blocks = (uint64_t)a.B * a.cache.Hkv * qtiles * split.n;
-  const uint64_t join = ((uint64_t)a.B * a.cache.Hkv * R + kThreads / (D / 4) - 1) / (kThreads / (D / 4));
-  if (blocks >= (1ull << 31) || join >= (1ull << 31)) return hipErrorInvalidValue;
-  if (qt == 1)
-    hipLaunchKernelGGL((verify_kernel<T, D, 1>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, split, qtiles);
+  constexpr int dtype = sizeof(T) == 2 ? SLA_DTYPE_BF16 : SLA_DTYPE_F32;
+  const int R = a.n * (a.Hq / a.cache.Hkv);
+  const Form f = form_of(R, dtype);
+  const Split split = plan(a, dtype);
+  hipError_t e;
+  constexpr int kSplitWaves = Tile<T, D>::kKeys / 16 < 4 ? Tile<T, D>::kKeys / 16 : 4;
+  if (f.wk > 1)
+    e = launch_form<T, D, 1, kSplitWaves>(a, Form{1, kSplitWaves, kSplitWaves}, split, s);
+  else if (f.qt == 1)
+    e = launch_form<T, D, 1, 1>(a, f, split, s);
+  else if constexpr (Tile<T, D>::kBf16)
+    e = launch_form<T, D, 2, 1>(a, f, split, s);
   else
-    hipLaunchKernelGGL((verify_kernel<T, D, 2>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, split, qtiles);
-  hipError_t e = hipGetLastError();
+    e = hipErrorInvalidConfiguration;
   if (e != hipSuccess || split.n == 1) return e;
+  const uint64_t join = ((uint64_t)a.B * a.cache.Hkv * R + kThreads / (D / 4) - 1) / (kThreads / (D / 4));
+  if (join >= (1ull << 31)) return hipErrorInvalidValue;
   hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)join), dim3(kThreads), 0, s, a, split);
   return hipGetLastError();
 }
@@ -468,7 +581,7 @@ hipError_t launch_t(const AttnVerifyArgs &a, hipStream_t s) {
 }  // namespace
 
 size_t attn_workspace_bytes(const AttnVerifyArgs &a, int dtype) {
-  const Split split = plan(a, tile_keys(a.cache.D, dtype));
+  const Split split = plan(a, dtype);
   if (split.n == 1) return 0;
   return (size_t)a.B * a.Hq * a.n * split.n * (a.cache.D + 2) * sizeof(float);
 }
