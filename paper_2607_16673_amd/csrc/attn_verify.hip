@@ -18,6 +18,7 @@
 // value per lane.  V^T comes out of the row-major tile by ds_read_b64_tr_b16.
 // fp32 activations use v_mfma_f32_16x16x4_f32 in the same arrangement, with
 // exact products.
+#include <stdlib.h>
 #include <type_traits>
 
 #include "attn_device.hpp"
@@ -26,7 +27,6 @@ namespace sla {
 namespace {
 
 constexpr int kThreads = 256;  // of the join kernel
-constexpr int kMaxWaves = 8;   // of the attention kernel
 constexpr int kQueries = 16;  // queries of one matrix tile
 constexpr float kSlack = 8.f;      // how far, in powers of two, a score may pass its softmax's reference
 constexpr float kNoScore = -3e38f;  // the reference before the first visible key
@@ -103,27 +103,46 @@ __device__ __forceinline__ f32x4 load4(const bf16 *p) {
 }
 __device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
 
+// Order of a block of fragment reads and the products that take them: AHEAD
+// fragments (READS reads each) first, then each fragment's PRODUCTS products
+// followed by the reads of the one AHEAD behind it.
+template <int AHEAD, int READS, int PRODUCTS, int FRAGS>
+__device__ __forceinline__ void pace() {
+  constexpr int kRead = 0x100, kMfma = 0x8;
+  constexpr int kFirst = AHEAD < FRAGS ? AHEAD : FRAGS;
+  __builtin_amdgcn_sched_group_barrier(kRead, kFirst * READS, 0);
+#pragma unroll
+  for (int f = 0; f < FRAGS; ++f) {
+    __builtin_amdgcn_sched_group_barrier(kMfma, PRODUCTS, 0);
+    if (f + kFirst < FRAGS) __builtin_amdgcn_sched_group_barrier(kRead, READS, 0);
+  }
+}
+
 // WK waves share a query's keys (each takes its part of every tile), the
 // workgroup's waves / WK groups of them take QT query tiles each.
-template <typename T, int D, int QT, int WK>
-__global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArgs a, Split split, int qtiles) {
+template <typename T, int D, int QT, int WK, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs a, Split split, int qtiles) {
   using L = Tile<T, D>;
   constexpr int kKeyTiles = L::kKeys / 16 / WK;  // of a wave
+  constexpr int kAhead = QT * D >= 512 ? 2 : 4;  // fragments read ahead of their products, as registers allow
   static_assert(kKeyTiles >= 1 && (!L::kBf16 || kKeyTiles == 1 || kKeyTiles % 2 == 0), "whole matrix tiles");
   __shared__ __attribute__((aligned(1024))) char stage[2][2 * L::kBytes];
   __shared__ uint64_t anc_s[kWave];
   __shared__ int bad_value;
 
   const int tid = threadIdx.x, lane = tid % kWave;
-  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), waves = blockDim.x / kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int g = lane / 16, col = lane % 16;
   const int n = a.n, Hkv = a.cache.Hkv, G = a.Hq / Hkv, R = n * G;
-  unsigned u = blockIdx.x;
+  // the query tiles of one key range, which read the same keys, are numbered
+  // back to back on one XCD
+  const unsigned turn = blockIdx.x / kXcdCount;
+  unsigned u = turn / qtiles * kXcdCount + blockIdx.x % kXcdCount;
+  const int qt0 = turn % qtiles * (WAVES / WK * QT * kQueries);
   const int sp = u % split.n;
   u /= split.n;
-  const int qt0 = u % qtiles * (waves / WK * QT * kQueries);
-  u /= qtiles;
   const int kv = u % Hkv, b = u / Hkv;
+  if (b >= a.B) return;
   const int shift = a.cache.page_shift;
 
   const int len = a.rows.len[b];
@@ -148,10 +167,9 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArg
   if (wave == 0) anc_s[lane] = node_ancestors(p, lane);
   if (tid == 0) bad_value = 0;
 
-  // tile loads.  Lane i < 16 holds the page of the tile's rows 16 i..16 i + 15;
+  // tile loads.  Lane i % 16 holds the page of the tile's rows 16 i..16 i + 15;
   // rows past the last one come from wherever the last page's row would be, and
   // are masked
-  const char *const kbase = static_cast<const char *>(a.cache.k), *const vbase = static_cast<const char *>(a.cache.v);
   const int last = (total - 1) >> shift;
   auto load_pages = [&](int k0) {
     return table[min((k0 + lane % 16 * 16) >> shift, last)];
@@ -159,13 +177,18 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArg
   const int load_row = lane / L::kCols, load_col = lane % L::kCols;
   auto load_tile = [&](int k0, int pages, char *dst) {
     pages = (unsigned)pages < (unsigned)a.cache.n_pages ? pages : 0;
-    for (int c = wave; c < L::kLoads; c += waves) {
-      const int first = c * L::kLoadRows;  // the load's first row in the tile
-      const int pg = __builtin_amdgcn_readlane(pages, first / 16);
-      const size_t off = (page_row(a.cache, pg, kv) + ((k0 + first) & ((1 << shift) - 1))) * L::kRow;
-      const int r = first + load_row;
-      load_lds16(kbase + off + load_row * L::kRow + ((load_col ^ L::swizzle_k(r)) * 16), dst + c * 1024);
-      load_lds16(vbase + off + load_row * L::kRow + ((load_col ^ L::swizzle_v(r)) * 16), dst + L::kBytes + c * 1024);
+    const uint64_t group = (page_row(a.cache, pages, kv) + ((k0 + lane % 16 * 16) & ((1 << shift) - 1))) * L::kRow;
+    const uint32_t lo = (uint32_t)group, hi = (uint32_t)(group >> 32);
+#pragma unroll
+    for (int i = 0; i < L::kLoads / WAVES; ++i) {
+      const int c = wave + i * WAVES, first = c * L::kLoadRows;  // the load, its first row in the tile
+      const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, first / 16) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane(lo, first / 16);
+      const int r = first % 16 + load_row;  // this lane's row of the group
+      load_lds16(static_cast<const char *>(a.cache.k) + off + (uint32_t)(r * L::kRow + (load_col ^ L::swizzle_k(r)) * 16),
+                 dst + c * 1024);
+      load_lds16(static_cast<const char *>(a.cache.v) + off + (uint32_t)(r * L::kRow + (load_col ^ L::swizzle_v(r)) * 16),
+                 dst + L::kBytes + c * 1024);
     }
   };
   int pages = load_pages(k_begin);
@@ -177,11 +200,11 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArg
   const int r0 = qt0 + wave / WK * (QT * kQueries), wk = wave % WK;
   const bool active = r0 < R;
   Frag<T, D> qf[QT];
-  uint64_t anc[QT];
+  int node[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int r = min(r0 + t * kQueries + col, R - 1);
-    anc[t] = anc_s[r / G];
+    node[t] = r / G;
     const T *q = static_cast<const T *>(a.q) + (((size_t)b * n + r / G) * a.Hq + (size_t)kv * G + r % G) * D;
     if constexpr (L::kBf16) {
 #pragma unroll
@@ -234,7 +257,7 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArg
       // a weight of 0 does not remove an infinity or a NaN from a product: a
       // draft row's are left out here and given to the queries that see the
       // row at the end (a committed row's reach every query in any case)
-      for (int c = tid; c < L::kBytes / 16; c += blockDim.x) {
+      for (int c = tid; c < L::kBytes / 16; c += WAVES * kWave) {
         const int k = k0 + c / L::kCols;
         if (k < len) continue;
         u32x4 *const piece = reinterpret_cast<u32x4 *>(cur + L::kBytes) + c;
@@ -252,30 +275,40 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArg
     // scores, transposed: keys 4 g + i of key tile kt, query col
     f32x4 s[QT][kKeyTiles];
 #pragma unroll
-    for (int kt = 0; kt < kKeyTiles; ++kt) {
+    for (int kt = 0; kt < kKeyTiles; ++kt)
 #pragma unroll
       for (int t = 0; t < QT; ++t) s[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const char *row = cur + k_row + kt * 16 * L::kRow;
-      if constexpr (L::kBf16) {
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (L::kBf16) {
+      constexpr int kChunks = D / 32, kFrags = kKeyTiles * kChunks;
+      bf16x8 kf[kFrags];
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(row + (c * 64 ^ k_piece));
+      for (int f = 0; f < kFrags; ++f)
+        kf[f] = *reinterpret_cast<const bf16x8 *>(cur + k_row + f / kChunks * 16 * L::kRow + (f % kChunks * 64 ^ k_piece));
 #pragma unroll
-          for (int t = 0; t < QT; ++t)
-            s[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t].x[c], s[t][kt], 0, 0, 0);
-        }
-      } else {
+      for (int f = 0; f < kFrags; ++f)
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-          const f32x4 kf = *reinterpret_cast<const f32x4 *>(row + (c * 64 ^ k_piece));
+        for (int t = 0; t < QT; ++t)
+          s[t][f / kChunks] =
+              __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[f], qf[t].x[f % kChunks], s[t][f / kChunks], 0, 0, 0);
+      pace<kAhead, 1, QT, kFrags>();
+    } else {
+      constexpr int kChunks = D / 16, kFrags = kKeyTiles * kChunks;
+      f32x4 kf[kFrags];
 #pragma unroll
-          for (int t = 0; t < QT; ++t)
+      for (int f = 0; f < kFrags; ++f)
+        kf[f] = *reinterpret_cast<const f32x4 *>(cur + k_row + f / kChunks * 16 * L::kRow + (f % kChunks * 64 ^ k_piece));
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              s[t][kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i], qf[t].x[c][i], s[t][kt], 0, 0, 0);
-        }
-      }
+      for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            s[t][f / kChunks] =
+                __builtin_amdgcn_mfma_f32_16x16x4f32(kf[f][i], qf[t].x[f % kChunks][i], s[t][f / kChunks], 0, 0, 0);
+      pace<2, 1, QT * 4, kFrags>();
     }
+    __builtin_amdgcn_sched_barrier(0);
     if (edge) {
 #pragma unroll
       for (int kt = 0; kt < kKeyTiles; ++kt) {
@@ -285,7 +318,8 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArg
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           const int up = -rel & 63;
-          uint64_t see = rel >= 0 ? anc[t] >> (rel & 63) : anc[t] << up | ((1ull << up) - 1);
+          const uint64_t anc = anc_s[node[t]];
+          uint64_t see = rel >= 0 ? anc >> (rel & 63) : anc << up | ((1ull << up) - 1);
           see = rel >= 64 ? 0 : rel <= -4 ? ~0ull : see;
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[t][kt][i] = (uint32_t)see >> i & 1 ? s[t][kt][i] : -INFINITY;
@@ -296,58 +330,69 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArg
     // more than 2^kSlack: weights stay below 2^kSlack, where fp32 sums and bf16
     // weights are as precise as below 1, and most tiles neither reduce a
     // maximum over the lanes nor rescale the output
+    float top[QT];
+    bool passed = false;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      float top = -INFINITY;
+      top[t] = -INFINITY;
 #pragma unroll
       for (int kt = 0; kt < kKeyTiles; ++kt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][kt][i]);
-      top *= scale;
-      if (wave_any(top - m[t] > kSlack)) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        top = fmaxf(top, m[t]);
-        const float shrink = __builtin_amdgcn_exp2f(m[t] - top);
-        m[t] = top;
+        for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], s[t][kt][i]);
+      top[t] *= scale;
+      passed |= top[t] - m[t] > kSlack;
+    }
+    if (wave_any(passed)) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        top[t] = fmaxf(top[t], __shfl_xor(top[t], 16));
+        top[t] = fmaxf(top[t], __shfl_xor(top[t], 32));
+        top[t] = fmaxf(top[t], m[t]);
+        const float shrink = __builtin_amdgcn_exp2f(m[t] - top[t]);
+        m[t] = top[t];
         l[t] *= shrink;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) o[t][d] *= shrink;
       }
-      float sum = 0.f;
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
 #pragma unroll
       for (int kt = 0; kt < kKeyTiles; ++kt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           s[t][kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][kt][i], scale, -m[t]));
-          sum += s[t][kt][i];
+          l[t] += s[t][kt][i];
         }
-      l[t] += sum;
-    }
 
     // O^T += V^T P^T
     if constexpr (L::kBf16 && kKeyTiles > 1) {
+      constexpr int kSteps = D / 16, kFrags = kKeyTiles / 2 * kSteps;
+      bf16x8 pf[QT][kKeyTiles / 2], vf[kFrags];
 #pragma unroll
-      for (int kp = 0; kp < kKeyTiles / 2; ++kp) {
-        bf16x8 pf[QT];
+      for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
+        for (int kp = 0; kp < kKeyTiles / 2; ++kp)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            pf[t][i] = static_cast<__bf16>(s[t][2 * kp][i]);
-            pf[t][4 + i] = static_cast<__bf16>(s[t][2 * kp + 1][i]);
+            pf[t][kp][i] = static_cast<__bf16>(s[t][2 * kp][i]);
+            pf[t][kp][4 + i] = static_cast<__bf16>(s[t][2 * kp + 1][i]);
           }
-        char *row = cur + v_row + kp * 32 * L::kRow;
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-          char *piece = row + (d * 32 ^ v_piece);
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)piece);
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(piece + 16 * L::kRow));
-          const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int t = 0; t < QT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], o[t][d], 0, 0, 0);
-        }
+      for (int f = 0; f < kFrags; ++f) {
+        char *piece = cur + v_row + f / kSteps * 32 * L::kRow + (f % kSteps * 32 ^ v_piece);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)piece);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(piece + 16 * L::kRow));
+        vf[f] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
       }
+#pragma unroll
+      for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+          o[t][f % kSteps] =
+              __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[f], pf[t][f / kSteps], o[t][f % kSteps], 0, 0, 0);
+      pace<kAhead, 2, QT, kFrags>();
     } else if constexpr (L::kBf16) {
       s16x4 pf[QT];
 #pragma unroll
@@ -392,11 +437,11 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArg
     // in each round
     float *const box = reinterpret_cast<float *>(stage[0]);
     constexpr int kBox = QT * (D / 16 * 4 + 2) * kWave;  // floats of a wave
-    static_assert(WK / 2 * kBox * 4 <= (int)sizeof(stage), "the first round's hand-over fits");
+    static_assert(WAVES / 2 * kBox * 4 <= (int)sizeof(stage), "the first round's hand-over fits");
 #pragma unroll
     for (int half = WK / 2; half >= 1; half /= 2) {
       __syncthreads();
-      float *const own = box + (wk % half) * kBox + lane;
+      float *const own = box + (wave / WK * (WK / 2) + wk % half) * kBox + lane;
       if (wk >= half && wk < 2 * half) {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
@@ -441,7 +486,7 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArg
         for (int t = 0; t < QT; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (!(fabsf(v[e]) < INFINITY) && (anc[t] >> (k - len)) & 1ull) o[t][d][e] += v[e];
+            if (!(fabsf(v[e]) < INFINITY) && (anc_s[node[t]] >> (k - len)) & 1ull) o[t][d][e] += v[e];
       }
     }
   }
@@ -474,35 +519,49 @@ __global__ __launch_bounds__(kMaxWaves * kWave) void verify_kernel(AttnVerifyArg
   }
 }
 
-// Joins the splits of a row: D / 4 lanes hold it, four elements each.
+// Joins the splits of a row.  `groups` groups of D / 4 lanes take every
+// groups-th split of a row, four elements a lane, and their sums meet in LDS.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split split) {
-  constexpr int kLanes = D / 4;
+__global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split split, int groups) {
+  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
+  __shared__ f32x4 part_x[kGroups][kLanes];
+  __shared__ float part_l[kGroups];
   const int n = a.n, Hkv = a.cache.Hkv, G = a.Hq / Hkv, R = n * G;
   const size_t rows = (size_t)a.B * Hkv * R;
-  const size_t i = (size_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
-  if (i >= rows) return;
-  const int r = i % R, kv = i / R % Hkv, b = i / R / Hkv;
+  const int slot = threadIdx.x / kLanes, grp = slot % groups, e = threadIdx.x % kLanes * 4;
+  const size_t i = (size_t)blockIdx.x * (kGroups / groups) + slot / groups;
+  const int r = i % R, kv = i / R % Hkv, b = min((int)(i / R / Hkv), a.B - 1);
   const int len = a.rows.len[b];
-  if (!length_ok(a.rows, a.cache.page_shift, len, n) || len > a.max_len) return;
-  const int total = len + n;
-  if (split.chunk >= total) return;  // written whole
-  const int parts = (total + split.chunk - 1) / split.chunk;
+  bool live = i < rows && length_ok(a.rows, a.cache.page_shift, len, n) && len <= a.max_len;
+  live = live && split.chunk < len + n;  // else written whole
+  const int parts = live ? (len + n + split.chunk - 1) / split.chunk : 0;
   const size_t first = ((size_t)b * Hkv + kv) * split.n * R + r;
   const float *ws = static_cast<const float *>(a.workspace);
   const float2 *ml = reinterpret_cast<const float2 *>(ws + rows * split.n * D);
-  const int e = threadIdx.x % kLanes * 4;
   float ref = kNoScore;
+#pragma unroll 8
   for (int s = 0; s < parts; ++s) ref = fmaxf(ref, ml[first + (size_t)s * R].x);
   float l = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < parts; ++s) {
+#pragma unroll 8
+  for (int s = grp; s < parts; s += groups) {
     const size_t row = first + (size_t)s * R;
     const float2 st = ml[row];
     const float w = __builtin_amdgcn_exp2f(st.x - ref);
     l = __builtin_fmaf(w, st.y, l);
     x += w * *reinterpret_cast<const f32x4 *>(ws + row * D + e);
   }
+  if (groups > 1) {  // (the same for the whole launch)
+    part_x[slot][e / 4] = x;
+    if (e == 0) part_l[slot] = l;
+    __syncthreads();
+    if (grp > 0) return;
+    for (int k = 1; k < groups; ++k) {
+      x += part_x[slot + k][e / 4];
+      l += part_l[slot + k];
+    }
+  }
+  if (!live) return;
   x *= 1.f / l;
   T *out = static_cast<T *>(a.out) + (((size_t)b * n + r / G) * a.Hq + (size_t)kv * G + r % G) * D + e;
   if constexpr (sizeof(T) == 2)
@@ -517,31 +576,34 @@ struct Form {
   int rows() const { return waves / wk * qt * kQueries; }
 };
 
-Form form_of(int R, int dtype) {
-  const int tiles = (R + kQueries - 1) / kQueries;
-  if (tiles == 1) return Form{1, 4, 4};
-  if (dtype == SLA_DTYPE_F32 || tiles <= 4) return Form{1, 1, tiles < kMaxWaves ? tiles : kMaxWaves};
-  return Form{2, 1, (tiles + 1) / 2 < kMaxWaves ? (tiles + 1) / 2 : kMaxWaves};
+Form form_of(int R, int D, int dtype) {
+  const int key_tiles = 16384 / (D * (dtype == SLA_DTYPE_BF16 ? 2 : 4)) / 16;
+  if (R <= kQueries) return Form{1, key_tiles < 4 ? key_tiles : 4, 4};
+  if (R <= 4 * kQueries) return Form{1, 1, 4};
+  if (dtype == SLA_DTYPE_F32) return Form{1, 1, 8};
+  return Form{2, 1, R <= 8 * kQueries ? 4 : 8};
 }
 
 int tile_keys(int D, int dtype) { return 16384 / (D * (dtype == SLA_DTYPE_BF16 ? 2 : 4)); }
 
 Split plan(const AttnVerifyArgs &a, int dtype) {
   const int R = a.n * (a.Hq / a.cache.Hkv), keys = tile_keys(a.cache.D, dtype);
-  const Form f = form_of(R, dtype);
+  const Form f = form_of(R, a.cache.D, dtype);
   const int64_t units = (int64_t)a.B * a.cache.Hkv * ((R + f.rows() - 1) / f.rows());
   const int64_t tiles = ((int64_t)a.max_len + a.n + keys - 1) / keys;
-  const int64_t want = ((f.waves > 4 ? 1 : 2) * device_cus() + units - 1) / units;
+  static const double X = getenv("SLA_X") ? atof(getenv("SLA_X")) : 2;
+  const int64_t want = ((int64_t)(X * device_cus()) + units - 1) / units;
   const int64_t per = (tiles + want - 1) / want;
   return Split{(int)((tiles + per - 1) / per), (int)(per * keys)};
 }
 
-template <typename T, int D, int QT, int WK>
+template <typename T, int D, int QT, int WK, int WAVES>
 hipError_t launch_form(const AttnVerifyArgs &a, const Form &f, const Split &split, hipStream_t s) {
   const int R = a.n * (a.Hq / a.cache.Hkv), qtiles = (R + f.rows() - 1) / f.rows();
-  const uint64_t blocks = (uint64_t)a.B * a.cache.Hkv * qtiles * split.n;
+  const uint64_t ranges = (uint64_t)a.B * a.cache.Hkv * split.n;
+  const uint64_t blocks = (ranges + kXcdCount - 1) / kXcdCount * kXcdCount * qtiles;
   if (blocks >= (1ull << 31)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((verify_kernel<T, D, QT, WK>), dim3((unsigned)blocks), dim3((unsigned)f.waves * kWave), 0, s, a, split,
+  hipLaunchKernelGGL((verify_kernel<T, D, QT, WK, WAVES>), dim3((unsigned)blocks), dim3(WAVES * kWave), 0, s, a, split,
                      qtiles);
   return hipGetLastError();
 }
@@ -550,22 +612,28 @@ template <typename T, int D>
 hipError_t launch_d(const AttnVerifyArgs &a, hipStream_t s) {
   constexpr int dtype = sizeof(T) == 2 ? SLA_DTYPE_BF16 : SLA_DTYPE_F32;
   const int R = a.n * (a.Hq / a.cache.Hkv);
-  const Form f = form_of(R, dtype);
+  const Form f = form_of(R, D, dtype);
   const Split split = plan(a, dtype);
   hipError_t e;
-  constexpr int kSplitWaves = Tile<T, D>::kKeys / 16 < 4 ? Tile<T, D>::kKeys / 16 : 4;
-  if (f.wk > 1)
-    e = launch_form<T, D, 1, kSplitWaves>(a, Form{1, kSplitWaves, kSplitWaves}, split, s);
-  else if (f.qt == 1)
-    e = launch_form<T, D, 1, 1>(a, f, split, s);
-  else if constexpr (Tile<T, D>::kBf16)
-    e = launch_form<T, D, 2, 1>(a, f, split, s);
+  constexpr int kKeyTiles = Tile<T, D>::kKeys / 16;
+  if (R <= kQueries)
+    e = launch_form<T, D, 1, kKeyTiles < 4 ? kKeyTiles : 4, 4>(a, f, split, s);
+  else if (R <= 4 * kQueries)
+    e = launch_form<T, D, 1, 1, 4>(a, f, split, s);
+  else if constexpr (!Tile<T, D>::kBf16)
+    e = launch_form<T, D, 1, 1, 8>(a, f, split, s);
+  else if (R <= 8 * kQueries)
+    e = launch_form<T, D, 2, 1, 4>(a, f, split, s);
   else
-    e = hipErrorInvalidConfiguration;
+    e = launch_form<T, D, 2, 1, 8>(a, f, split, s);
   if (e != hipSuccess || split.n == 1) return e;
-  const uint64_t join = ((uint64_t)a.B * a.cache.Hkv * R + kThreads / (D / 4) - 1) / (kThreads / (D / 4));
+  constexpr int kGroups = kThreads / (D / 4);
+  int groups = 1;  // two splits or more for each group
+  while (groups < kGroups && groups * 4 <= split.n) groups *= 2;
+  const uint64_t rows = (uint64_t)a.B * a.cache.Hkv * R;
+  const uint64_t join = (rows * groups + kGroups - 1) / kGroups;
   if (join >= (1ull << 31)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)join), dim3(kThreads), 0, s, a, split);
+  hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)join), dim3(kThreads), 0, s, a, split, groups);
   return hipGetLastError();
 }
 
