@@ -389,8 +389,8 @@ int sla_tree_mask_to_parent_host(const uint64_t *mask, int32_t n_nodes, int32_t 
  * layer's.  Row r of sequence b is row r mod page_size of page
  * page_table[b][r / page_size], in every head; rows 0..cache_len[b]-1 are the
  * committed tokens and row cache_len[b] + j is draft node j's.  Entries of
- * the page table past a sequence's last row are not read.  Sequences may share
- * pages; no two of one call may write the same row.
+ * the page table past a sequence's last row may hold anything.  Sequences may
+ * share pages; no two of one call may write the same row.
  *
  * Positions.  Node j stands at position cache_len[b] + depth(j) - 1, depth as
  * in sla_topology (a root has depth 1): siblings share a position.

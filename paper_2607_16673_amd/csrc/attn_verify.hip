@@ -103,6 +103,25 @@ __device__ __forceinline__ f32x4 load4(const bf16 *p) {
 }
 __device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
 
+// The workspace of a split launch: unnormalised outputs [B][Hkv][splits][R][D],
+// their reference and sum [B][Hkv][splits][R], the errors of each range [B][splits].
+__host__ __device__ inline size_t split_rows(const AttnVerifyArgs &a, const Split &s, int R) {
+  return (size_t)a.B * a.cache.Hkv * s.n * R;
+}
+__device__ __forceinline__ float2 *split_stats(const AttnVerifyArgs &a, const Split &s, int R) {
+  return reinterpret_cast<float2 *>(static_cast<float *>(a.workspace) + split_rows(a, s, R) * a.cache.D);
+}
+__device__ __forceinline__ int32_t *split_errors(const AttnVerifyArgs &a, const Split &s, int R) {
+  return reinterpret_cast<int32_t *>(split_stats(a, s, R) + split_rows(a, s, R));
+}
+
+// A lane's 32-bit offset from a wave-uniform base, kept apart from it: added up
+// ahead of a loop, every such address would hold two registers through it.
+__device__ __forceinline__ uint32_t own_offset(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Order of a block of fragment reads and the products that take them: AHEAD
 // fragments (READS reads each) first, then each fragment's PRODUCTS products
 // followed by the reads of the one AHEAD behind it.
@@ -145,38 +164,31 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
   if (b >= a.B) return;
   const int shift = a.cache.page_shift;
 
+  // the range's pages come with the sequence's length: a row past the last one
+  // lies in whatever page the table names there (page 0 if it names none), and
+  // is masked
+  const int k_begin = sp * split.chunk;
+  const int32_t *const table = a.rows.table + (size_t)b * a.rows.max_pages;
+  auto load_pages = [&](int k0) { return table[min((k0 + lane % 16 * 16) >> shift, a.rows.max_pages - 1)]; };
+  int pages = load_pages(k_begin);
   const int len = a.rows.len[b];
-  const int p = lane < n ? a.parent[(size_t)b * n + lane] : -1;
-  int err = SLA_OK;
-  if (!parents_ok(p, n, lane, a.chain)) err = SLA_ERR_TOPOLOGY;
-  else if (!length_ok(a.rows, shift, len, n) || len > a.max_len) err = SLA_ERR_LENGTH;
-  const int32_t *table = a.rows.table + (size_t)b * a.rows.max_pages;
-  const int total = err == SLA_OK ? len + n : 0;
-  if (a.status && kv == 0 && qt0 == 0 && sp == 0 && wave == 0) {
-    if (err == SLA_OK) {
-      bool bad = false;
-      for (int i = lane; i <= (total - 1) >> shift; i += kWave) bad |= (unsigned)table[i] >= (unsigned)a.cache.n_pages;
-      if (wave_any(bad)) err = SLA_ERR_PAGE;
-    }
-    if (lane == 0) a.status[b] = err;
+  const bool reports = kv == 0 && qt0 == 0;  // this workgroup tells of its range's errors
+  int32_t *const err = split.n > 1 ? split_errors(a, split, R) + (size_t)b * split.n + sp : a.status ? a.status + b : nullptr;
+  if (!length_ok(a.rows, shift, len, n) || len > a.max_len) {
+    if (reports && err && tid == 0) *err = SLA_ERR_LENGTH;
+    return;
   }
-  if (err == SLA_ERR_TOPOLOGY || err == SLA_ERR_LENGTH) return;
-  const int k_begin = sp * split.chunk, k_end = min(k_begin + split.chunk, total);
+  const int total = len + n, k_end = min(k_begin + split.chunk, total);
   if (k_begin >= k_end) return;
+  bool bad_page = false, bad_topology = false;
 
-  if (wave == 0) anc_s[lane] = node_ancestors(p, lane);
-  if (tid == 0) bad_value = 0;
-
-  // tile loads.  Lane i % 16 holds the page of the tile's rows 16 i..16 i + 15;
-  // rows past the last one come from wherever the last page's row would be, and
-  // are masked
-  const int last = (total - 1) >> shift;
-  auto load_pages = [&](int k0) {
-    return table[min((k0 + lane % 16 * 16) >> shift, last)];
-  };
+  // tile loads; lane i % 16 holds the page of the tile's rows 16 i..16 i + 15
   const int load_row = lane / L::kCols, load_col = lane % L::kCols;
   auto load_tile = [&](int k0, int pages, char *dst) {
-    pages = (unsigned)pages < (unsigned)a.cache.n_pages ? pages : 0;
+    if ((unsigned)pages >= (unsigned)a.cache.n_pages) {
+      bad_page |= k0 + lane % 16 * 16 < k_end && lane % 16 * 16 < L::kKeys;
+      pages = 0;
+    }
     const uint64_t group = (page_row(a.cache, pages, kv) + ((k0 + lane % 16 * 16) & ((1 << shift) - 1))) * L::kRow;
     const uint32_t lo = (uint32_t)group, hi = (uint32_t)(group >> 32);
 #pragma unroll
@@ -185,18 +197,16 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
       const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, first / 16) << 32 |
                            (uint32_t)__builtin_amdgcn_readlane(lo, first / 16);
       const int r = first % 16 + load_row;  // this lane's row of the group
-      load_lds16(static_cast<const char *>(a.cache.k) + off + (uint32_t)(r * L::kRow + (load_col ^ L::swizzle_k(r)) * 16),
+      load_lds16(static_cast<const char *>(a.cache.k) + off + own_offset(r * L::kRow + (load_col ^ L::swizzle_k(r)) * 16),
                  dst + c * 1024);
-      load_lds16(static_cast<const char *>(a.cache.v) + off + (uint32_t)(r * L::kRow + (load_col ^ L::swizzle_v(r)) * 16),
+      load_lds16(static_cast<const char *>(a.cache.v) + off + own_offset(r * L::kRow + (load_col ^ L::swizzle_v(r)) * 16),
                  dst + L::kBytes + c * 1024);
     }
   };
-  int pages = load_pages(k_begin);
   load_tile(k_begin, pages, stage[0]);
   pages = load_pages(k_begin + L::kKeys);
 
-  // this wave's queries, and their ancestors
-  __syncthreads();
+  // this wave's queries
   const int r0 = qt0 + wave / WK * (QT * kQueries), wk = wave % WK;
   const bool active = r0 < R;
   Frag<T, D> qf[QT];
@@ -246,6 +256,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
   const int v_piece = L::kBf16 ? ((col % 4 / 2) ^ L::swizzle_v(v_in)) * 16 + col % 2 * 8
                                : ((col / 4) ^ L::swizzle_v(v_in)) * 16 + col % 4 * 4;
 
+  if (tid == 0) bad_value = 0;  // (the first tile's barrier follows)
   // attends to the staged tile `cur` while the next one's loads run
   auto step = [&](int k0, char *__restrict__ cur, char *__restrict__ next) {
     if (k0 + L::kKeys < k_end) {
@@ -254,6 +265,11 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
     }
     const bool edge = k0 + L::kKeys > len;  // the tile reaches into the draft
     if (edge) {
+      if (wave == 0 && (k0 == k_begin || k0 <= len)) {  // the range's first such tile
+        const int p = lane < n ? a.parent[(size_t)b * n + lane] : -1;
+        bad_topology = !parents_ok(p, n, lane, a.chain);
+        anc_s[lane] = bad_topology ? 0 : node_ancestors(p, lane);
+      }
       // a weight of 0 does not remove an infinity or a NaN from a product: a
       // draft row's are left out here and given to the queries that see the
       // row at the end (a committed row's reach every query in any case)
@@ -427,6 +443,10 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
     step(k0, stage[buf], stage[buf ^ 1]);
   }
 
+  if (reports && wave == 0 && err) {
+    bad_page = wave_any(bad_page);
+    if (lane == 0) *err = bad_topology ? SLA_ERR_TOPOLOGY : bad_page ? SLA_ERR_PAGE : SLA_OK;
+  }
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     l[t] += __shfl_xor(l[t], 16);
@@ -513,53 +533,86 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
       float *out = ws + row * D + 4 * g;
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4 *>(out + d * 16) = o[t][d];
-      if (g == 0)
-        *reinterpret_cast<float2 *>(ws + (size_t)a.B * Hkv * split.n * R * D + row * 2) = make_float2(m[t], l[t]);
+      if (g == 0) split_stats(a, split, R)[row] = make_float2(m[t], l[t]);
     }
   }
 }
 
-// Joins the splits of a row.  `groups` groups of D / 4 lanes take every
-// groups-th split of a row, four elements a lane, and their sums meet in LDS.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split split, int groups) {
-  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
-  __shared__ f32x4 part_x[kGroups][kLanes];
-  __shared__ float part_l[kGroups];
+// Joins the splits of a row.  GROUPS groups of D / 4 lanes, four elements a
+// lane, take every GROUPS-th split of a row, kBatch of them read at a time, and
+// meet in LDS.
+template <typename T, int D, int GROUPS>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split split) {
+  constexpr int kLanes = D / 4, kSlots = kThreads / kLanes, kBatch = 4;
+  __shared__ f32x4 part_x[GROUPS > 1 ? kSlots : 1][kLanes];
+  __shared__ float2 part_ml[GROUPS > 1 ? kSlots : 1];
   const int n = a.n, Hkv = a.cache.Hkv, G = a.Hq / Hkv, R = n * G;
   const size_t rows = (size_t)a.B * Hkv * R;
-  const int slot = threadIdx.x / kLanes, grp = slot % groups, e = threadIdx.x % kLanes * 4;
-  const size_t i = (size_t)blockIdx.x * (kGroups / groups) + slot / groups;
+  const int slot = threadIdx.x / kLanes, grp = slot % GROUPS, e = threadIdx.x % kLanes * 4;
+  const size_t i = (size_t)blockIdx.x * (kSlots / GROUPS) + slot / GROUPS;
   const int r = i % R, kv = i / R % Hkv, b = min((int)(i / R / Hkv), a.B - 1);
   const int len = a.rows.len[b];
-  bool live = i < rows && length_ok(a.rows, a.cache.page_shift, len, n) && len <= a.max_len;
-  live = live && split.chunk < len + n;  // else written whole
-  const int parts = live ? (len + n + split.chunk - 1) / split.chunk : 0;
-  const size_t first = ((size_t)b * Hkv + kv) * split.n * R + r;
-  const float *ws = static_cast<const float *>(a.workspace);
-  const float2 *ml = reinterpret_cast<const float2 *>(ws + rows * split.n * D);
-  float ref = kNoScore;
-#pragma unroll 8
-  for (int s = 0; s < parts; ++s) ref = fmaxf(ref, ml[first + (size_t)s * R].x);
-  float l = 0.f;
+  const bool fits = length_ok(a.rows, a.cache.page_shift, len, n) && len <= a.max_len;
+  const bool live = i < rows && fits && split.chunk < len + n;  // else written whole
+  const int ranges = fits ? (len + n + split.chunk - 1) / split.chunk : 1, parts = live ? ranges : 0;
+  const float *const ws = static_cast<const float *>(a.workspace) + ((((size_t)b * Hkv + kv) * split.n) * R + r) * D + e;
+  const float2 *const ml = split_stats(a, split, R) + (((size_t)b * Hkv + kv) * split.n) * R + r;
+  float ref = kNoScore, l = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int s = grp; s < parts; s += groups) {
-    const size_t row = first + (size_t)s * R;
-    const float2 st = ml[row];
-    const float w = __builtin_amdgcn_exp2f(st.x - ref);
-    l = __builtin_fmaf(w, st.y, l);
-    x += w * *reinterpret_cast<const f32x4 *>(ws + row * D + e);
+  for (int s0 = grp; s0 < parts; s0 += kBatch * GROUPS) {
+    float2 st[kBatch];
+    f32x4 y[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const size_t s = min(s0 + k * GROUPS, parts - 1);
+      st[k] = ml[s * R];
+      y[k] = *reinterpret_cast<const f32x4 *>(ws + s * R * D);
+    }
+    float top = ref;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) top = fmaxf(top, st[k].x);
+    const float shrink = __builtin_amdgcn_exp2f(ref - top);
+    ref = top;
+    l *= shrink;
+    x *= shrink;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (s0 + k * GROUPS < parts) {
+        const float w = __builtin_amdgcn_exp2f(st[k].x - ref);
+        l = __builtin_fmaf(w, st[k].y, l);
+        x += w * y[k];
+      }
   }
-  if (groups > 1) {  // (the same for the whole launch)
+  if constexpr (GROUPS > 1) {
     part_x[slot][e / 4] = x;
-    if (e == 0) part_l[slot] = l;
+    if (e == 0) part_ml[slot] = make_float2(ref, l);
     __syncthreads();
     if (grp > 0) return;
-    for (int k = 1; k < groups; ++k) {
-      x += part_x[slot + k][e / 4];
-      l += part_l[slot + k];
+    float top = ref;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) top = fmaxf(top, part_ml[slot + k].x);
+    const float w0 = __builtin_amdgcn_exp2f(ref - top);
+    l *= w0;
+    x *= w0;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) {
+      const float w = __builtin_amdgcn_exp2f(part_ml[slot + k].x - top);
+      l = __builtin_fmaf(w, part_ml[slot + k].y, l);
+      x += w * part_x[slot + k][e / 4];
     }
+  }
+  if (a.status && i < rows && kv == 0 && r == 0) {  // (the row's lanes together)
+    bool topology = false, page = false, length = false;
+    for (int s = e / 4; s < ranges; s += kLanes) {
+      const int err = split_errors(a, split, R)[(size_t)b * split.n + s];
+      topology |= err == SLA_ERR_TOPOLOGY;
+      length |= err == SLA_ERR_LENGTH;
+      page |= err == SLA_ERR_PAGE;
+    }
+    topology = wave_any(topology);
+    length = wave_any(length);
+    page = wave_any(page);
+    if (e == 0) a.status[b] = topology ? SLA_ERR_TOPOLOGY : length ? SLA_ERR_LENGTH : page ? SLA_ERR_PAGE : SLA_OK;
   }
   if (!live) return;
   x *= 1.f / l;
@@ -591,8 +644,8 @@ Split plan(const AttnVerifyArgs &a, int dtype) {
   const Form f = form_of(R, a.cache.D, dtype);
   const int64_t units = (int64_t)a.B * a.cache.Hkv * ((R + f.rows() - 1) / f.rows());
   const int64_t tiles = ((int64_t)a.max_len + a.n + keys - 1) / keys;
-  static const double X = getenv("SLA_X") ? atof(getenv("SLA_X")) : 2;
-  const int64_t want = ((int64_t)(X * device_cus()) + units - 1) / units;
+  static const double X = getenv("SLA_X") ? atof(getenv("SLA_X")) : 1;
+  const int64_t want = ((int64_t)(X * device_cus() * (8 / f.waves)) + units - 1) / units;
   const int64_t per = (tiles + want - 1) / want;
   return Split{(int)((tiles + per - 1) / per), (int)(per * keys)};
 }
@@ -605,6 +658,15 @@ hipError_t launch_form(const AttnVerifyArgs &a, const Form &f, const Split &spli
   if (blocks >= (1ull << 31)) return hipErrorInvalidValue;
   hipLaunchKernelGGL((verify_kernel<T, D, QT, WK, WAVES>), dim3((unsigned)blocks), dim3(WAVES * kWave), 0, s, a, split,
                      qtiles);
+  return hipGetLastError();
+}
+
+template <typename T, int D, int GROUPS>
+hipError_t launch_join(const AttnVerifyArgs &a, const Split &split, hipStream_t s) {
+  constexpr int kRows = kThreads / (D / 4) / GROUPS;  // of a workgroup
+  const uint64_t rows = (uint64_t)a.B * a.n * a.Hq, blocks = (rows + kRows - 1) / kRows;
+  if (blocks >= (1ull << 31)) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((join_kernel<T, D, GROUPS>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, split);
   return hipGetLastError();
 }
 
@@ -627,14 +689,10 @@ hipError_t launch_d(const AttnVerifyArgs &a, hipStream_t s) {
   else
     e = launch_form<T, D, 2, 1, 8>(a, f, split, s);
   if (e != hipSuccess || split.n == 1) return e;
-  constexpr int kGroups = kThreads / (D / 4);
-  int groups = 1;  // two splits or more for each group
-  while (groups < kGroups && groups * 4 <= split.n) groups *= 2;
-  const uint64_t rows = (uint64_t)a.B * a.cache.Hkv * R;
-  const uint64_t join = (rows * groups + kGroups - 1) / kGroups;
-  if (join >= (1ull << 31)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)join), dim3(kThreads), 0, s, a, split, groups);
-  return hipGetLastError();
+  // a group for every four splits, up to the whole workgroup
+  if (split.n <= 4) return launch_join<T, D, 1>(a, split, s);
+  if (split.n <= 8) return launch_join<T, D, 2>(a, split, s);
+  return launch_join<T, D, kThreads / (D / 4)>(a, split, s);
 }
 
 template <typename T>
@@ -651,7 +709,8 @@ hipError_t launch_t(const AttnVerifyArgs &a, hipStream_t s) {
 size_t attn_workspace_bytes(const AttnVerifyArgs &a, int dtype) {
   const Split split = plan(a, dtype);
   if (split.n == 1) return 0;
-  return (size_t)a.B * a.Hq * a.n * split.n * (a.cache.D + 2) * sizeof(float);
+  return split_rows(a, split, a.n * (a.Hq / a.cache.Hkv)) * (a.cache.D + 2) * sizeof(float) +
+         (size_t)a.B * split.n * sizeof(int32_t);
 }
 
 hipError_t launch_attn_verify(const AttnVerifyArgs &a, int dtype, hipStream_t s) {
