@@ -36,6 +36,8 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(4))) int32_t const_int;  // read by scalar loads
+
 
 // A tile of keys and values in LDS, 16 KB each, filled by direct loads: 64
 // lanes bring 1 KB, one 16-byte piece a lane, to consecutive addresses.  Piece
@@ -122,6 +124,10 @@ __device__ __forceinline__ uint32_t own_offset(uint32_t x) {
   return x;
 }
 
+// Where the piece at `offset` of a row lies for a lane whose swizzle is `lane`
+// (below 256): a few exclusive-ors for a row, the rest in the reads' immediates.
+__device__ __forceinline__ int place(int offset, int lane) { return (offset % 256 ^ lane) + offset / 256 * 256; }
+
 // Order of a block of fragment reads and the products that take them: AHEAD
 // fragments (READS reads each) first, then each fragment's PRODUCTS products
 // followed by the reads of the one AHEAD behind it.
@@ -143,11 +149,12 @@ template <typename T, int D, int QT, int WK, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs a, Split split, int qtiles) {
   using L = Tile<T, D>;
   constexpr int kKeyTiles = L::kKeys / 16 / WK;  // of a wave
-  constexpr int kAhead = QT * D >= 512 ? 2 : 4;  // fragments read ahead of their products, as registers allow
+  constexpr int kAhead = QT * D >= 320 ? (L::kBf16 ? 4 : 2) : 8;  // fragments read ahead of their products, as registers allow
   static_assert(kKeyTiles >= 1 && (!L::kBf16 || kKeyTiles == 1 || kKeyTiles % 2 == 0), "whole matrix tiles");
   __shared__ __attribute__((aligned(1024))) char stage[2][2 * L::kBytes];
   __shared__ uint64_t anc_s[kWave];
   __shared__ int bad_value;
+  __shared__ bool bad_page_s[WAVES];
 
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -164,13 +171,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
   if (b >= a.B) return;
   const int shift = a.cache.page_shift;
 
-  // the range's pages come with the sequence's length: a row past the last one
-  // lies in whatever page the table names there (page 0 if it names none), and
-  // is masked
   const int k_begin = sp * split.chunk;
-  const int32_t *const table = a.rows.table + (size_t)b * a.rows.max_pages;
-  auto load_pages = [&](int k0) { return table[min((k0 + lane % 16 * 16) >> shift, a.rows.max_pages - 1)]; };
-  int pages = load_pages(k_begin);
   const int len = a.rows.len[b];
   const bool reports = kv == 0 && qt0 == 0;  // this workgroup tells of its range's errors
   int32_t *const err = split.n > 1 ? split_errors(a, split, R) + (size_t)b * split.n + sp : a.status ? a.status + b : nullptr;
@@ -182,29 +183,49 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
   if (k_begin >= k_end) return;
   bool bad_page = false, bad_topology = false;
 
-  // tile loads; lane i % 16 holds the page of the tile's rows 16 i..16 i + 15
-  const int load_row = lane / L::kCols, load_col = lane % L::kCols;
-  auto load_tile = [&](int k0, int pages, char *dst) {
-    if ((unsigned)pages >= (unsigned)a.cache.n_pages) {
-      bad_page |= k0 + lane % 16 * 16 < k_end && lane % 16 * 16 < L::kKeys;
-      pages = 0;
-    }
-    const uint64_t group = (page_row(a.cache, pages, kv) + ((k0 + lane % 16 * 16) & ((1 << shift) - 1))) * L::kRow;
-    const uint32_t lo = (uint32_t)group, hi = (uint32_t)(group >> 32);
+  // A tile goes through registers: its rows are read while the tile before is
+  // worked on and written to LDS after that.  A wave's load i brings rows
+  // `first`.. of the 16 that share a page.  The page comes from the table by a
+  // scalar load, for it is the same in all lanes; a row past the last one lies
+  // in whatever page the table names there (page 0 if it names none), and is
+  // masked.
+  constexpr int kOwnLoads = L::kLoads / WAVES;
+  const const_int *const table = (const const_int *)(uintptr_t)(a.rows.table + (size_t)b * a.rows.max_pages);
+  // Keys and values travel together, 32 KB of a workgroup's reads at a time,
+  // but where the registers hold one of them only (head size 256, two query
+  // tiles a wave): there the values are read when the keys have been written.
+  constexpr bool kTogether = QT * D < (L::kBf16 ? 512 : 320);
+  u32x4 rows[kTogether ? 2 : 1][kOwnLoads];
+  constexpr int kV = kTogether ? 1 : 0;  // the values' rows
+  auto read_rows = [&](int k0, bool keys, bool values) __attribute__((always_inline)) {
+    const uint32_t own = own_offset(lane * 16);
 #pragma unroll
-    for (int i = 0; i < L::kLoads / WAVES; ++i) {
-      const int c = wave + i * WAVES, first = c * L::kLoadRows;  // the load, its first row in the tile
-      const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, first / 16) << 32 |
-                           (uint32_t)__builtin_amdgcn_readlane(lo, first / 16);
-      const int r = first % 16 + load_row;  // this lane's row of the group
-      load_lds16(static_cast<const char *>(a.cache.k) + off + own_offset(r * L::kRow + (load_col ^ L::swizzle_k(r)) * 16),
-                 dst + c * 1024);
-      load_lds16(static_cast<const char *>(a.cache.v) + off + own_offset(r * L::kRow + (load_col ^ L::swizzle_v(r)) * 16),
-                 dst + L::kBytes + c * 1024);
+    for (int i = 0; i < kOwnLoads; ++i) {
+      const int first = (wave + i * WAVES) * L::kLoadRows, k = k0 + first / 16 * 16;
+      int pg = table[min(k >> shift, a.rows.max_pages - 1)];
+      if ((unsigned)pg >= (unsigned)a.cache.n_pages) {
+        bad_page |= k < k_end;
+        pg = 0;
+      }
+      const uint64_t off = (page_row(a.cache, pg, kv) + ((k & ((1 << shift) - 1)) + first % 16)) * L::kRow;
+      if (keys) rows[0][i] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.cache.k) + off + own);
+      if (values) rows[kV][i] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.cache.v) + off + own);
     }
   };
-  load_tile(k_begin, pages, stage[0]);
-  pages = load_pages(k_begin + L::kKeys);
+  auto write_rows = [&](char *dst, bool keys, bool values) __attribute__((always_inline)) {
+    const int own = kTogether ? lane : own_offset(lane);
+#pragma unroll
+    for (int i = 0; i < kOwnLoads; ++i) {
+      const int r = (wave + i * WAVES) * L::kLoadRows + own / L::kCols, piece = own % L::kCols;
+      if (keys) *reinterpret_cast<u32x4 *>(dst + r * L::kRow + (piece ^ L::swizzle_k(r)) * 16) = rows[0][i];
+      if (values) *reinterpret_cast<u32x4 *>(dst + L::kBytes + r * L::kRow + (piece ^ L::swizzle_v(r)) * 16) = rows[kV][i];
+    }
+  };
+  read_rows(k_begin, true, kTogether);
+  if (!kTogether) {
+    write_rows(stage[0], true, false);
+    read_rows(k_begin, false, true);
+  }
 
   // this wave's queries
   const int r0 = qt0 + wave / WK * (QT * kQueries), wk = wave % WK;
@@ -257,12 +278,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
                                : ((col / 4) ^ L::swizzle_v(v_in)) * 16 + col % 4 * 4;
 
   if (tid == 0) bad_value = 0;  // (the first tile's barrier follows)
-  // attends to the staged tile `cur` while the next one's loads run
-  auto step = [&](int k0, char *__restrict__ cur, char *__restrict__ next) {
-    if (k0 + L::kKeys < k_end) {
-      load_tile(k0 + L::kKeys, pages, next);
-      pages = load_pages(k0 + 2 * L::kKeys);
-    }
+  // attends to the staged tile `cur`
+  auto step = [&](int k0, char *cur, char *next) {
     const bool edge = k0 + L::kKeys > len;  // the tile reaches into the draft
     if (edge) {
       if (wave == 0 && (k0 == k_begin || k0 <= len)) {  // the range's first such tile
@@ -286,166 +303,183 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
       }
       __syncthreads();
     }
-    if (!active) return;
-
-    // scores, transposed: keys 4 g + i of key tile kt, query col
     f32x4 s[QT][kKeyTiles];
-#pragma unroll
-    for (int kt = 0; kt < kKeyTiles; ++kt)
-#pragma unroll
-      for (int t = 0; t < QT; ++t) s[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    __builtin_amdgcn_sched_barrier(0);
-    if constexpr (L::kBf16) {
-      constexpr int kChunks = D / 32, kFrags = kKeyTiles * kChunks;
-      bf16x8 kf[kFrags];
-#pragma unroll
-      for (int f = 0; f < kFrags; ++f)
-        kf[f] = *reinterpret_cast<const bf16x8 *>(cur + k_row + f / kChunks * 16 * L::kRow + (f % kChunks * 64 ^ k_piece));
-#pragma unroll
-      for (int f = 0; f < kFrags; ++f)
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-          s[t][f / kChunks] =
-              __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[f], qf[t].x[f % kChunks], s[t][f / kChunks], 0, 0, 0);
-      pace<kAhead, 1, QT, kFrags>();
-    } else {
-      constexpr int kChunks = D / 16, kFrags = kKeyTiles * kChunks;
-      f32x4 kf[kFrags];
-#pragma unroll
-      for (int f = 0; f < kFrags; ++f)
-        kf[f] = *reinterpret_cast<const f32x4 *>(cur + k_row + f / kChunks * 16 * L::kRow + (f % kChunks * 64 ^ k_piece));
-#pragma unroll
-      for (int f = 0; f < kFrags; ++f)
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            s[t][f / kChunks] =
-                __builtin_amdgcn_mfma_f32_16x16x4f32(kf[f][i], qf[t].x[f % kChunks][i], s[t][f / kChunks], 0, 0, 0);
-      pace<2, 1, QT * 4, kFrags>();
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if (edge) {
-#pragma unroll
-      for (int kt = 0; kt < kKeyTiles; ++kt) {
-        // bit i: the query sees key 4 g + i, draft node rel + i.  Bits of nodes
-        // past the draft are clear in every mask.
-        const int rel = k0 + (wk * kKeyTiles + kt) * 16 + 4 * g - len;
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          const int up = -rel & 63;
-          const uint64_t anc = anc_s[node[t]];
-          uint64_t see = rel >= 0 ? anc >> (rel & 63) : anc << up | ((1ull << up) - 1);
-          see = rel >= 64 ? 0 : rel <= -4 ? ~0ull : see;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[t][kt][i] = (uint32_t)see >> i & 1 ? s[t][kt][i] : -INFINITY;
-        }
-      }
-    }
-    // softmax against a reference that only moves when a score exceeds it by
-    // more than 2^kSlack: weights stay below 2^kSlack, where fp32 sums and bf16
-    // weights are as precise as below 1, and most tiles neither reduce a
-    // maximum over the lanes nor rescale the output
-    float top[QT];
-    bool passed = false;
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      top[t] = -INFINITY;
+    if (active) {
+      const int k_own = own_offset(k_piece);
+      // scores, transposed: keys 4 g + i of key tile kt, query col
 #pragma unroll
       for (int kt = 0; kt < kKeyTiles; ++kt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], s[t][kt][i]);
-      top[t] *= scale;
-      passed |= top[t] - m[t] > kSlack;
+        for (int t = 0; t < QT; ++t) s[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (L::kBf16) {
+        constexpr int kChunks = D / 32, kFrags = kKeyTiles * kChunks;
+        bf16x8 kf[kFrags];
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f)
+          kf[f] = *reinterpret_cast<const bf16x8 *>(cur + k_row + f / kChunks * 16 * L::kRow + place(f % kChunks * 64, k_own));
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+            s[t][f / kChunks] =
+                __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[f], qf[t].x[f % kChunks], s[t][f / kChunks], 0, 0, 0);
+        pace<kAhead, 1, QT, kFrags>();
+      } else {
+        constexpr int kChunks = D / 16, kFrags = kKeyTiles * kChunks;
+        f32x4 kf[kFrags];
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f)
+          kf[f] = *reinterpret_cast<const f32x4 *>(cur + k_row + f / kChunks * 16 * L::kRow + place(f % kChunks * 64, k_own));
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              s[t][f / kChunks] =
+                  __builtin_amdgcn_mfma_f32_16x16x4f32(kf[f][i], qf[t].x[f % kChunks][i], s[t][f / kChunks], 0, 0, 0);
+        pace<(kAhead < 4 ? kAhead : 4), 1, QT * 4, kFrags>();
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (edge) {
+#pragma unroll
+        for (int kt = 0; kt < kKeyTiles; ++kt) {
+          // bit i: the query sees key 4 g + i, draft node rel + i.  Bits of nodes
+          // past the draft are clear in every mask.
+          const int rel = k0 + (wk * kKeyTiles + kt) * 16 + 4 * g - len;
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+            const int up = -rel & 63;
+            const uint64_t anc = anc_s[node[t]];
+            uint64_t see = rel >= 0 ? anc >> (rel & 63) : anc << up | ((1ull << up) - 1);
+            see = rel >= 64 ? 0 : rel <= -4 ? ~0ull : see;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[t][kt][i] = (uint32_t)see >> i & 1 ? s[t][kt][i] : -INFINITY;
+          }
+        }
+      }
     }
-    if (wave_any(passed)) {
+    if (!kTogether && k0 + L::kKeys < k_end) {
+      write_rows(next, true, false);
+      read_rows(k0 + L::kKeys, false, true);
+    }
+    if (active) {
+      // softmax against a reference that only moves when a score exceeds it by
+      // more than 2^kSlack: weights stay below 2^kSlack, where fp32 sums and bf16
+      // weights are as precise as below 1, and most tiles neither reduce a
+      // maximum over the lanes nor rescale the output
+      float top[QT];
+      bool passed = false;
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        top[t] = fmaxf(top[t], __shfl_xor(top[t], 16));
-        top[t] = fmaxf(top[t], __shfl_xor(top[t], 32));
-        top[t] = fmaxf(top[t], m[t]);
-        const float shrink = __builtin_amdgcn_exp2f(m[t] - top[t]);
-        m[t] = top[t];
-        l[t] *= shrink;
+        top[t] = -INFINITY;
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) o[t][d] *= shrink;
+        for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], s[t][kt][i]);
+        top[t] *= scale;
+        passed |= top[t] - m[t] > kSlack;
       }
-    }
+      if (wave_any(passed)) {
 #pragma unroll
-    for (int t = 0; t < QT; ++t)
+        for (int t = 0; t < QT; ++t) {
+          top[t] = fmaxf(top[t], __shfl_xor(top[t], 16));
+          top[t] = fmaxf(top[t], __shfl_xor(top[t], 32));
+          top[t] = fmaxf(top[t], m[t]);
+          const float shrink = __builtin_amdgcn_exp2f(m[t] - top[t]);
+          m[t] = top[t];
+          l[t] *= shrink;
 #pragma unroll
-      for (int kt = 0; kt < kKeyTiles; ++kt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[t][kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][kt][i], scale, -m[t]));
-          l[t] += s[t][kt][i];
+          for (int d = 0; d < D / 16; ++d) o[t][d] *= shrink;
         }
-
-    // O^T += V^T P^T
-    if constexpr (L::kBf16 && kKeyTiles > 1) {
-      constexpr int kSteps = D / 16, kFrags = kKeyTiles / 2 * kSteps;
-      bf16x8 pf[QT][kKeyTiles / 2], vf[kFrags];
+      }
 #pragma unroll
       for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int kp = 0; kp < kKeyTiles / 2; ++kp)
+        for (int kt = 0; kt < kKeyTiles; ++kt)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            pf[t][kp][i] = static_cast<__bf16>(s[t][2 * kp][i]);
-            pf[t][kp][4 + i] = static_cast<__bf16>(s[t][2 * kp + 1][i]);
+            s[t][kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][kt][i], scale, -m[t]));
+            l[t] += s[t][kt][i];
           }
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int f = 0; f < kFrags; ++f) {
-        char *piece = cur + v_row + f / kSteps * 32 * L::kRow + (f % kSteps * 32 ^ v_piece);
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)piece);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(piece + 16 * L::kRow));
-        vf[f] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      }
-#pragma unroll
-      for (int f = 0; f < kFrags; ++f)
+    }
+    if (active) {
+      const int v_own = own_offset(v_piece);
+      // O^T += V^T P^T
+      if constexpr (L::kBf16 && kKeyTiles > 1) {
+        constexpr int kSteps = D / 16, kFrags = kKeyTiles / 2 * kSteps;
+        bf16x8 pf[QT][kKeyTiles / 2], vf[kFrags];
 #pragma unroll
         for (int t = 0; t < QT; ++t)
-          o[t][f % kSteps] =
-              __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[f], pf[t][f / kSteps], o[t][f % kSteps], 0, 0, 0);
-      pace<kAhead, 2, QT, kFrags>();
-    } else if constexpr (L::kBf16) {
-      s16x4 pf[QT];
 #pragma unroll
-      for (int t = 0; t < QT; ++t)
+          for (int kp = 0; kp < kKeyTiles / 2; ++kp)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pf[t][i] = __builtin_bit_cast(short, static_cast<__bf16>(s[t][0][i]));
+            for (int i = 0; i < 4; ++i) {
+              pf[t][kp][i] = static_cast<__bf16>(s[t][2 * kp][i]);
+              pf[t][kp][4 + i] = static_cast<__bf16>(s[t][2 * kp + 1][i]);
+            }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) {
-        const s16x4 vf = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(cur + v_row + (d * 32 ^ v_piece)));
+        for (int f = 0; f < kFrags; ++f) {
+          char *piece = cur + v_row + f / kSteps * 32 * L::kRow + place(f % kSteps * 32, v_own);
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)piece);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(piece + 16 * L::kRow));
+          vf[f] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
 #pragma unroll
-        for (int t = 0; t < QT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, pf[t], o[t][d], 0, 0, 0);
+        for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+            o[t][f % kSteps] =
+                __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[f], pf[t][f / kSteps], o[t][f % kSteps], 0, 0, 0);
+        pace<kAhead, 2, QT, kFrags>();
+      } else if constexpr (L::kBf16) {
+        s16x4 pf[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) pf[t][i] = __builtin_bit_cast(short, static_cast<__bf16>(s[t][0][i]));
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+          const s16x4 vf = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(cur + v_row + place(d * 32, v_own)));
+#pragma unroll
+          for (int t = 0; t < QT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, pf[t], o[t][d], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int kt = 0; kt < kKeyTiles; ++kt)
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float vf = *reinterpret_cast<const float *>(cur + v_row + (kt * 16 + i) * L::kRow + place(d * 64, v_own));
+#pragma unroll
+              for (int t = 0; t < QT; ++t)
+                o[t][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, s[t][kt][i], o[t][d], 0, 0, 0);
+            }
       }
-    } else {
-#pragma unroll
-      for (int kt = 0; kt < kKeyTiles; ++kt)
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float vf = *reinterpret_cast<const float *>(cur + v_row + (kt * 16 + i) * L::kRow + (d * 64 ^ v_piece));
-#pragma unroll
-            for (int t = 0; t < QT; ++t)
-              o[t][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, s[t][kt][i], o[t][d], 0, 0, 0);
-          }
     }
   };
 
+  write_rows(stage[0], kTogether, true);
+  if (k_begin + L::kKeys < k_end) read_rows(k_begin + L::kKeys, true, kTogether);
   int buf = 0;
   for (int k0 = k_begin; k0 < k_end; k0 += L::kKeys, buf ^= 1) {
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's part of the tile has landed
-    __syncthreads();                     // and every other wave's; the other buffer is free
+    __syncthreads();  // the tile is whole, and the other buffer free
     step(k0, stage[buf], stage[buf ^ 1]);
+    if (k0 + L::kKeys < k_end) write_rows(stage[buf ^ 1], kTogether, true);
+    if (k0 + 2 * L::kKeys < k_end) read_rows(k0 + 2 * L::kKeys, true, kTogether);
   }
 
-  if (reports && wave == 0 && err) {
-    bad_page = wave_any(bad_page);
-    if (lane == 0) *err = bad_topology ? SLA_ERR_TOPOLOGY : bad_page ? SLA_ERR_PAGE : SLA_OK;
+  if (reports && err) {
+    if (lane == 0) bad_page_s[wave] = bad_page;
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) bad_page |= bad_page_s[w];
+      *err = bad_topology ? SLA_ERR_TOPOLOGY : bad_page ? SLA_ERR_PAGE : SLA_OK;
+    }
   }
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -623,31 +657,52 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
     *reinterpret_cast<f32x4 *>(out) = x;
 }
 
-// How a workgroup is laid out for R rows of a kv head.
+// How a workgroup is laid out for the rows of a kv head: `qt` query tiles a
+// wave, `wk` waves that share a query's keys, `waves` in all.
 struct Form {
   int qt, wk, waves;
-  int rows() const { return waves / wk * qt * kQueries; }
+  int tiles() const { return waves / wk * qt; }
+  int rows() const { return tiles() * kQueries; }
 };
 
-Form form_of(int R, int D, int dtype) {
-  const int key_tiles = 16384 / (D * (dtype == SLA_DTYPE_BF16 ? 2 : 4)) / 16;
-  if (R <= kQueries) return Form{1, key_tiles < 4 ? key_tiles : 4, 4};
-  if (R <= 4 * kQueries) return Form{1, 1, 4};
-  if (dtype == SLA_DTYPE_F32) return Form{1, 1, 8};
-  return Form{2, 1, R <= 8 * kQueries ? 4 : 8};
+// Key-split forms, in which every wave holds all of a workgroup's queries and
+// takes its share of each tile's keys, up to this many query tiles: as many as
+// the registers hold next to a tile in flight.  A fragment is read from LDS by
+// one wave only, and the waves have equal work whatever the number of rows.
+template <typename T, int D>
+constexpr int key_split_tiles() {
+  return sizeof(T) == 2 ? (D == 64 ? 4 : D == 128 ? 3 : 1) : (D == 64 ? 5 : D == 128 ? 2 : 0);
 }
 
-int tile_keys(int D, int dtype) { return 16384 / (D * (dtype == SLA_DTYPE_BF16 ? 2 : 4)); }
+template <typename T, int D>
+Form form_of(int R) {
+  constexpr int kKeyTiles = Tile<T, D>::kKeys / 16, kSplit = kKeyTiles < 4 ? kKeyTiles : 4;
+  constexpr int kMost = key_split_tiles<T, D>();
+  const int tiles = (R + kQueries - 1) / kQueries;
+  if (tiles <= kMost) return Form{tiles, kSplit, 4};
+  if (sizeof(T) == 4) {
+    // fp32 products bound it: queries in equal parts rather than full tiles
+    if (kMost == 0) return Form{1, 1, 8};
+    constexpr int kGroups = 4 / kSplit;  // groups of waves in a workgroup
+    const int blocks = (tiles + kMost * kGroups - 1) / (kMost * kGroups);
+    return Form{(tiles + blocks * kGroups - 1) / (blocks * kGroups), kSplit, 4};
+  }
+  if (tiles <= 4) return Form{1, 1, 4};
+  if (D == 256 && tiles <= 8) return Form{1, 1, 8};
+  return Form{2, 1, tiles <= 8 ? 4 : 8};
+}
 
-Split plan(const AttnVerifyArgs &a, int dtype) {
-  const int R = a.n * (a.Hq / a.cache.Hkv), keys = tile_keys(a.cache.D, dtype);
-  const Form f = form_of(R, a.cache.D, dtype);
+template <typename T, int D>
+Split plan(const AttnVerifyArgs &a) {
+  constexpr int kKeys = Tile<T, D>::kKeys;
+  const int R = a.n * (a.Hq / a.cache.Hkv);
+  const Form f = form_of<T, D>(R);
   const int64_t units = (int64_t)a.B * a.cache.Hkv * ((R + f.rows() - 1) / f.rows());
-  const int64_t tiles = ((int64_t)a.max_len + a.n + keys - 1) / keys;
+  const int64_t tiles = ((int64_t)a.max_len + a.n + kKeys - 1) / kKeys;
   static const double X = getenv("SLA_X") ? atof(getenv("SLA_X")) : 1;
   const int64_t want = ((int64_t)(X * device_cus() * (8 / f.waves)) + units - 1) / units;
   const int64_t per = (tiles + want - 1) / want;
-  return Split{(int)((tiles + per - 1) / per), (int)(per * keys)};
+  return Split{(int)((tiles + per - 1) / per), (int)(per * kKeys)};
 }
 
 template <typename T, int D, int QT, int WK, int WAVES>
@@ -672,22 +727,26 @@ hipError_t launch_join(const AttnVerifyArgs &a, const Split &split, hipStream_t 
 
 template <typename T, int D>
 hipError_t launch_d(const AttnVerifyArgs &a, hipStream_t s) {
-  constexpr int dtype = sizeof(T) == 2 ? SLA_DTYPE_BF16 : SLA_DTYPE_F32;
-  const int R = a.n * (a.Hq / a.cache.Hkv);
-  const Form f = form_of(R, D, dtype);
-  const Split split = plan(a, dtype);
-  hipError_t e;
-  constexpr int kKeyTiles = Tile<T, D>::kKeys / 16;
-  if (R <= kQueries)
-    e = launch_form<T, D, 1, kKeyTiles < 4 ? kKeyTiles : 4, 4>(a, f, split, s);
-  else if (R <= 4 * kQueries)
-    e = launch_form<T, D, 1, 1, 4>(a, f, split, s);
-  else if constexpr (!Tile<T, D>::kBf16)
-    e = launch_form<T, D, 1, 1, 8>(a, f, split, s);
-  else if (R <= 8 * kQueries)
-    e = launch_form<T, D, 2, 1, 4>(a, f, split, s);
-  else
-    e = launch_form<T, D, 2, 1, 8>(a, f, split, s);
+  constexpr int kKeyTiles = Tile<T, D>::kKeys / 16, kSplit = kKeyTiles < 4 ? kKeyTiles : 4;
+  constexpr int kMost = key_split_tiles<T, D>();
+  const Form f = form_of<T, D>(a.n * (a.Hq / a.cache.Hkv));
+  const Split split = plan<T, D>(a);
+  hipError_t e = hipErrorInvalidConfiguration;
+  if (f.wk == kSplit && f.waves == 4 && f.qt <= kMost) {
+    if constexpr (kMost >= 1) if (f.qt == 1) e = launch_form<T, D, 1, kSplit, 4>(a, f, split, s);
+    if constexpr (kMost >= 2) if (f.qt == 2) e = launch_form<T, D, 2, kSplit, 4>(a, f, split, s);
+    if constexpr (kMost >= 3) if (f.qt == 3) e = launch_form<T, D, 3, kSplit, 4>(a, f, split, s);
+    if constexpr (kMost >= 4) if (f.qt == 4) e = launch_form<T, D, 4, kSplit, 4>(a, f, split, s);
+    if constexpr (kMost >= 5) if (f.qt == 5) e = launch_form<T, D, 5, kSplit, 4>(a, f, split, s);
+  } else if constexpr (sizeof(T) == 4) {
+    if constexpr (kMost == 0) e = launch_form<T, D, 1, 1, 8>(a, f, split, s);
+  } else if (f.waves == 8) {
+    if constexpr (D == 256) if (f.qt == 1) e = launch_form<T, D, 1, 1, 8>(a, f, split, s);
+    if (f.qt == 2) e = launch_form<T, D, 2, 1, 8>(a, f, split, s);
+  } else {
+    if constexpr (kMost < 4) if (f.qt == 1) e = launch_form<T, D, 1, 1, 4>(a, f, split, s);
+    if constexpr (D < 256) if (f.qt == 2) e = launch_form<T, D, 2, 1, 4>(a, f, split, s);
+  }
   if (e != hipSuccess || split.n == 1) return e;
   // a group for every four splits, up to the whole workgroup
   if (split.n <= 4) return launch_join<T, D, 1>(a, split, s);
@@ -707,7 +766,10 @@ hipError_t launch_t(const AttnVerifyArgs &a, hipStream_t s) {
 }  // namespace
 
 size_t attn_workspace_bytes(const AttnVerifyArgs &a, int dtype) {
-  const Split split = plan(a, dtype);
+  const bool bf = dtype == SLA_DTYPE_BF16;
+  const Split split = a.cache.D == 64    ? (bf ? plan<bf16, 64>(a) : plan<float, 64>(a))
+                      : a.cache.D == 128 ? (bf ? plan<bf16, 128>(a) : plan<float, 128>(a))
+                                         : (bf ? plan<bf16, 256>(a) : plan<float, 256>(a));
   if (split.n == 1) return 0;
   return split_rows(a, split, a.n * (a.Hq / a.cache.Hkv)) * (a.cache.D + 2) * sizeof(float) +
          (size_t)a.B * split.n * sizeof(int32_t);
