@@ -18,8 +18,7 @@
 // value per lane.  V^T comes out of the row-major tile by ds_read_b64_tr_b16.
 // fp32 activations use v_mfma_f32_16x16x4_f32 in the same arrangement, with
 // exact products.
-#include <stdlib.h>
-#include <type_traits>
+#include <algorithm>
 
 #include "attn_device.hpp"
 
@@ -60,9 +59,13 @@ struct Tile {
   }
 };
 
+// How a launch's keys are divided.  Every sequence has as many ranges of whole
+// tiles as its length asks for, so that the ranges of a batch are about equally
+// long: the tiles of all sequences over `share`, at least, is a range's most,
+// and `ranges` bounds how many there are.  share 0: one range a sequence.
 struct Split {
-  int n;      // splits of every unit
-  int chunk;  // keys of a split, a multiple of the tile
+  int share, ranges;
+  bool fine;  // as many ranges as `ranges` allows, rather than as few as `share` asks for
 };
 
 // A query fragment: the B operand of S^T = K Q^T for 16 queries.
@@ -105,16 +108,132 @@ __device__ __forceinline__ f32x4 load4(const bf16 *p) {
 }
 __device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
 
-// The workspace of a split launch: unnormalised outputs [B][Hkv][splits][R][D],
-// their reference and sum [B][Hkv][splits][R], the errors of each range [B][splits].
+// The workspace of a split launch: unnormalised outputs [Hkv][ranges][R][D],
+// their reference and sum [Hkv][ranges][R], each sequence's first range and how
+// many it has [B], each range's error [ranges].
 __host__ __device__ inline size_t split_rows(const AttnVerifyArgs &a, const Split &s, int R) {
-  return (size_t)a.B * a.cache.Hkv * s.n * R;
+  return (size_t)a.cache.Hkv * s.ranges * R;
 }
 __device__ __forceinline__ float2 *split_stats(const AttnVerifyArgs &a, const Split &s, int R) {
   return reinterpret_cast<float2 *>(static_cast<float *>(a.workspace) + split_rows(a, s, R) * a.cache.D);
 }
+__device__ __forceinline__ int2 *split_ranges(const AttnVerifyArgs &a, const Split &s, int R) {
+  return reinterpret_cast<int2 *>(split_stats(a, s, R) + split_rows(a, s, R));
+}
 __device__ __forceinline__ int32_t *split_errors(const AttnVerifyArgs &a, const Split &s, int R) {
-  return reinterpret_cast<int32_t *>(split_stats(a, s, R) + split_rows(a, s, R));
+  return reinterpret_cast<int32_t *>(split_ranges(a, s, R) + a.B);
+}
+
+// Sum over the lanes up to this one, by rows of 16, then across them.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast 31 into rows 2 and 3
+  return x;
+}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), kWave - 1); }
+
+struct Range {
+  int b, part, parts, first;  // the sequence, which of its ranges, how many, the number of the first
+};
+
+// The range number `item` of a launch: false if there are fewer.  All threads
+// of a workgroup call it.  The longest range is the smallest of kTries lengths,
+// from the tiles over `ranges` to the tiles over `share`, that makes no more
+// than `ranges` of them; the last always does, for a sequence's last range is
+// the only one that may be shorter.
+template <int KEYS, int WAVES>
+__device__ __forceinline__ bool pick_range(const AttnVerifyArgs &a, const Split &s, int item, Range &r) {
+  constexpr int kTries = 4;
+  __shared__ uint32_t sum_s[2][WAVES];
+  __shared__ int count_s[kTries][WAVES], scan_s[WAVES];
+  __shared__ Range found_s;
+  auto tiles_of = [&](int b) {
+    const int len = a.rows.len[b];
+    return length_ok(a.rows, a.cache.page_shift, len, a.n) && len <= a.max_len ? (len + a.n + KEYS - 1) / KEYS : 0;
+  };
+  auto over = [](int tiles, int most) { return max((tiles + most - 1) / most, 1); };  // a bad length has one range, too
+  if (s.share == 0) {
+    r = Range{item, 0, 1, item};
+    return item < a.B;
+  }
+  if (a.B == 1) {
+    const int tiles = tiles_of(0);
+    r = Range{0, item, over(tiles, over(tiles, s.ranges)), 0};
+    return item < r.parts;
+  }
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int own = (a.B + WAVES * kWave - 1) / (WAVES * kWave);  // sequences of a thread
+  const int b0 = min(tid * own, a.B), b1 = min(b0 + own, a.B);
+  // (a batch's tiles pass 32 bits: summed by halves of 16)
+  uint32_t low = 0, high = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int t = tiles_of(b);
+    low += t & 0xffff;
+    high += t >> 16;
+  }
+  low = wave_sum(low);
+  high = wave_sum(high);
+  if (lane == 0) {
+    sum_s[0][wave] = low;
+    sum_s[1][wave] = high;
+  }
+  __syncthreads();
+  unsigned long long sum = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) sum += sum_s[0][w] + ((unsigned long long)sum_s[1][w] << 16);
+  int most[kTries], count[kTries] = {};
+  const int hi = (int)((sum + s.share - 1) / s.share), lo = s.fine ? (int)((sum + s.ranges - 1) / s.ranges) : hi;
+#pragma unroll
+  for (int i = 0; i < kTries; ++i) most[i] = max(lo + (int)((long long)(hi - lo) * i / (kTries - 1)), 1);
+  for (int b = b0; b < b1; ++b) {
+    const int t = tiles_of(b);
+#pragma unroll
+    for (int i = 0; i < kTries; ++i) count[i] += over(t, most[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kTries; ++i) {
+    const int total = wave_sum(count[i]);
+    if (lane == 0) count_s[i][wave] = total;
+  }
+  __syncthreads();
+  int longest = most[kTries - 1], mine = count[kTries - 1], all = 0;
+  bool chosen = false;
+#pragma unroll
+  for (int i = 0; i < kTries; ++i) {
+    int c = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) c += count_s[i][w];
+    if (!chosen && (c <= s.ranges || i == kTries - 1)) {
+      chosen = true;
+      longest = most[i];
+      mine = count[i];
+      all = c;
+    }
+  }
+  if (item >= all) return false;
+  int before = wave_scan(mine);  // ranges of this thread's sequences and of those in front of them
+  if (lane == kWave - 1) scan_s[wave] = before;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w)
+    if (w < wave) before += scan_s[w];
+  int first = before - mine;
+  if (item >= first && item < before)
+    for (int b = b0; b < b1; ++b) {
+      const int parts = over(tiles_of(b), longest);
+      if (item < first + parts) {
+        found_s = Range{b, item - first, parts, first};
+        break;
+      }
+      first += parts;
+    }
+  __syncthreads();
+  r = found_s;
+  return true;
 }
 
 // A lane's 32-bit offset from a wave-uniform base, kept apart from it: added up
@@ -165,22 +284,25 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
   const unsigned turn = blockIdx.x / kXcdCount;
   unsigned u = turn / qtiles * kXcdCount + blockIdx.x % kXcdCount;
   const int qt0 = turn % qtiles * (WAVES / WK * QT * kQueries);
-  const int sp = u % split.n;
-  u /= split.n;
-  const int kv = u % Hkv, b = u / Hkv;
-  if (b >= a.B) return;
+  const int kv = u % Hkv;
+  Range range;
+  if (!pick_range<L::kKeys, WAVES>(a, split, u / Hkv, range)) return;
+  const int b = __builtin_amdgcn_readfirstlane(range.b), parts = __builtin_amdgcn_readfirstlane(range.parts);
+  const int part = __builtin_amdgcn_readfirstlane(range.part);
+  const int item = __builtin_amdgcn_readfirstlane(range.first) + part;
   const int shift = a.cache.page_shift;
 
-  const int k_begin = sp * split.chunk;
   const int len = a.rows.len[b];
-  const bool reports = kv == 0 && qt0 == 0;  // this workgroup tells of its range's errors
-  int32_t *const err = split.n > 1 ? split_errors(a, split, R) + (size_t)b * split.n + sp : a.status ? a.status + b : nullptr;
+  const bool reports = kv == 0 && qt0 == 0;  // this workgroup tells of its range and the range's errors
+  int32_t *const err = split.share ? split_errors(a, split, R) + item : a.status ? a.status + b : nullptr;
+  if (reports && split.share && part == 0 && tid == 0) split_ranges(a, split, R)[b] = make_int2(item, parts);
   if (!length_ok(a.rows, shift, len, n) || len > a.max_len) {
     if (reports && err && tid == 0) *err = SLA_ERR_LENGTH;
     return;
   }
-  const int total = len + n, k_end = min(k_begin + split.chunk, total);
-  if (k_begin >= k_end) return;
+  const int total = len + n, tiles = (total + L::kKeys - 1) / L::kKeys;
+  const int k_begin = (int)((long long)tiles * part / parts) * L::kKeys;
+  const int k_end = min((int)((long long)tiles * (part + 1) / parts) * L::kKeys, total);
   bool bad_page = false, bad_topology = false;
 
   // A tile goes through registers: its rows are read while the tile before is
@@ -488,18 +610,17 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
   }
   if constexpr (WK > 1) {
     // the waves of a query join theirs, half of them handing over to the rest
-    // in each round
+    // in each round, one query tile at a time
     float *const box = reinterpret_cast<float *>(stage[0]);
-    constexpr int kBox = QT * (D / 16 * 4 + 2) * kWave;  // floats of a wave
+    constexpr int kBox = (D / 16 * 4 + 2) * kWave;  // floats of a wave
     static_assert(WAVES / 2 * kBox * 4 <= (int)sizeof(stage), "the first round's hand-over fits");
 #pragma unroll
     for (int half = WK / 2; half >= 1; half /= 2) {
-      __syncthreads();
-      float *const own = box + (wave / WK * (WK / 2) + wk % half) * kBox + lane;
-      if (wk >= half && wk < 2 * half) {
+      float *const x = box + (wave / WK * (WK / 2) + wk % half) * kBox + lane;
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          float *x = own + t * (D / 16 * 4 + 2) * kWave;
+      for (int t = 0; t < QT; ++t) {
+        __syncthreads();
+        if (wk >= half && wk < 2 * half) {
           x[0] = m[t];
           x[kWave] = l[t];
 #pragma unroll
@@ -507,12 +628,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[(2 + d * 4 + i) * kWave] = o[t][d][i];
         }
-      }
-      __syncthreads();
-      if (wk < half) {
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          const float *x = own + t * (D / 16 * 4 + 2) * kWave;
+        __syncthreads();
+        if (wk < half) {
           const float top = fmaxf(m[t], x[0]);
           const float w0 = __builtin_amdgcn_exp2f(m[t] - top), w1 = __builtin_amdgcn_exp2f(x[0] - top);
           m[t] = top;
@@ -545,7 +662,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
     }
   }
 
-  const bool whole = split.chunk >= total;  // no other workgroup has keys of these rows
+  const bool whole = parts == 1;  // no other workgroup has keys of these rows
   float *const ws = static_cast<float *>(a.workspace);
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -563,7 +680,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
           *reinterpret_cast<f32x4 *>(out + d * 16) = x;
       }
     } else {
-      const size_t row = (((size_t)b * Hkv + kv) * split.n + sp) * R + r;
+      const size_t row = ((size_t)kv * split.ranges + item) * R + r;
       float *out = ws + row * D + 4 * g;
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4 *>(out + d * 16) = o[t][d];
@@ -585,12 +702,12 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
   const int slot = threadIdx.x / kLanes, grp = slot % GROUPS, e = threadIdx.x % kLanes * 4;
   const size_t i = (size_t)blockIdx.x * (kSlots / GROUPS) + slot / GROUPS;
   const int r = i % R, kv = i / R % Hkv, b = min((int)(i / R / Hkv), a.B - 1);
-  const int len = a.rows.len[b];
-  const bool fits = length_ok(a.rows, a.cache.page_shift, len, n) && len <= a.max_len;
-  const bool live = i < rows && fits && split.chunk < len + n;  // else written whole
-  const int ranges = fits ? (len + n + split.chunk - 1) / split.chunk : 1, parts = live ? ranges : 0;
-  const float *const ws = static_cast<const float *>(a.workspace) + ((((size_t)b * Hkv + kv) * split.n) * R + r) * D + e;
-  const float2 *const ml = split_stats(a, split, R) + (((size_t)b * Hkv + kv) * split.n) * R + r;
+  const int2 own = split_ranges(a, split, R)[b];
+  const bool live = i < rows && own.y > 1;  // else written whole
+  const int parts = live ? own.y : 0;
+  const size_t row0 = ((size_t)kv * split.ranges + own.x) * R + r;
+  const float *const ws = static_cast<const float *>(a.workspace) + row0 * D + e;
+  const float2 *const ml = split_stats(a, split, R) + row0;
   float ref = kNoScore, l = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = grp; s0 < parts; s0 += kBatch * GROUPS) {
@@ -637,8 +754,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
   }
   if (a.status && i < rows && kv == 0 && r == 0) {  // (the row's lanes together)
     bool topology = false, page = false, length = false;
-    for (int s = e / 4; s < ranges; s += kLanes) {
-      const int err = split_errors(a, split, R)[(size_t)b * split.n + s];
+    for (int s = e / 4; s < own.y; s += kLanes) {
+      const int err = split_errors(a, split, R)[own.x + s];
       topology |= err == SLA_ERR_TOPOLOGY;
       length |= err == SLA_ERR_LENGTH;
       page |= err == SLA_ERR_PAGE;
@@ -697,18 +814,22 @@ Split plan(const AttnVerifyArgs &a) {
   constexpr int kKeys = Tile<T, D>::kKeys;
   const int R = a.n * (a.Hq / a.cache.Hkv);
   const Form f = form_of<T, D>(R);
-  const int64_t units = (int64_t)a.B * a.cache.Hkv * ((R + f.rows() - 1) / f.rows());
-  const int64_t tiles = ((int64_t)a.max_len + a.n + kKeys - 1) / kKeys;
-  static const double X = getenv("SLA_X") ? atof(getenv("SLA_X")) : 1;
-  const int64_t want = ((int64_t)(X * device_cus() * (8 / f.waves)) + units - 1) / units;
-  const int64_t per = (tiles + want - 1) / want;
-  return Split{(int)((tiles + per - 1) / per), (int)(per * kKeys)};
+  const int64_t tiles = ((int64_t)a.max_len + a.n + kKeys - 1) / kKeys;  // of the longest sequence there may be
+  if (tiles == 1) return Split{0, a.B, false};
+  // workgroups that run at once, and the ranges that makes of the batch's keys
+  const int64_t slots = (int64_t)device_cus() * (8 / f.waves);
+  const int64_t want = std::max<int64_t>(1, slots / ((int64_t)a.cache.Hkv * ((R + f.rows() - 1) / f.rows())));
+  for (int64_t ranges = want; ranges <= 2 * want; ranges += want)
+    if (ranges > a.B) return Split{(int)(ranges - a.B), (int)std::min<int64_t>(ranges, a.B * tiles), true};
+  // more sequences than that: only one much longer than a workgroup's even share is divided
+  const int64_t share = (want + 1) / 2;
+  return Split{(int)std::max<int64_t>(share, 1), (int)std::min<int64_t>(share + 1 + a.B, a.B * tiles), false};
 }
 
 template <typename T, int D, int QT, int WK, int WAVES>
 hipError_t launch_form(const AttnVerifyArgs &a, const Form &f, const Split &split, hipStream_t s) {
   const int R = a.n * (a.Hq / a.cache.Hkv), qtiles = (R + f.rows() - 1) / f.rows();
-  const uint64_t ranges = (uint64_t)a.B * a.cache.Hkv * split.n;
+  const uint64_t ranges = (uint64_t)split.ranges * a.cache.Hkv;
   const uint64_t blocks = (ranges + kXcdCount - 1) / kXcdCount * kXcdCount * qtiles;
   if (blocks >= (1ull << 31)) return hipErrorInvalidValue;
   hipLaunchKernelGGL((verify_kernel<T, D, QT, WK, WAVES>), dim3((unsigned)blocks), dim3(WAVES * kWave), 0, s, a, split,
@@ -747,10 +868,10 @@ hipError_t launch_d(const AttnVerifyArgs &a, hipStream_t s) {
     if constexpr (kMost < 4) if (f.qt == 1) e = launch_form<T, D, 1, 1, 4>(a, f, split, s);
     if constexpr (D < 256) if (f.qt == 2) e = launch_form<T, D, 2, 1, 4>(a, f, split, s);
   }
-  if (e != hipSuccess || split.n == 1) return e;
-  // a group for every four splits, up to the whole workgroup
-  if (split.n <= 4) return launch_join<T, D, 1>(a, split, s);
-  if (split.n <= 8) return launch_join<T, D, 2>(a, split, s);
+  if (e != hipSuccess || split.share == 0) return e;
+  // a group for every four ranges of a sequence of mean length, up to the whole workgroup
+  if (split.ranges <= 4 * (int64_t)a.B) return launch_join<T, D, 1>(a, split, s);
+  if (split.ranges <= 8 * (int64_t)a.B) return launch_join<T, D, 2>(a, split, s);
   return launch_join<T, D, kThreads / (D / 4)>(a, split, s);
 }
 
@@ -770,9 +891,9 @@ size_t attn_workspace_bytes(const AttnVerifyArgs &a, int dtype) {
   const Split split = a.cache.D == 64    ? (bf ? plan<bf16, 64>(a) : plan<float, 64>(a))
                       : a.cache.D == 128 ? (bf ? plan<bf16, 128>(a) : plan<float, 128>(a))
                                          : (bf ? plan<bf16, 256>(a) : plan<float, 256>(a));
-  if (split.n == 1) return 0;
+  if (split.share == 0) return 0;
   return split_rows(a, split, a.n * (a.Hq / a.cache.Hkv)) * (a.cache.D + 2) * sizeof(float) +
-         (size_t)a.B * split.n * sizeof(int32_t);
+         (size_t)a.B * sizeof(int2) + (size_t)split.ranges * sizeof(int32_t);
 }
 
 hipError_t launch_attn_verify(const AttnVerifyArgs &a, int dtype, hipStream_t s) {
