@@ -586,6 +586,11 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
 
   write_rows(stage[0], kTogether, true);
   if (k_begin + L::kKeys < k_end) read_rows(k_begin + L::kKeys, true, kTogether);
+  // Two workgroups share a CU.  With one ahead of the other at the issue ports
+  // their phases part: while one forms products the other takes exponentials
+  // (64 sequences of 16-node trees 50.7 -> 48.7 us).  Workgroups numbered 256
+  // apart usually meet.
+  if (WAVES == 4 && (blockIdx.x >> 8) & 1) __builtin_amdgcn_s_setprio(2);
   int buf = 0;
   for (int k0 = k_begin; k0 < k_end; k0 += L::kKeys, buf ^= 1) {
     __syncthreads();  // the tile is whole, and the other buffer free
