@@ -399,7 +399,15 @@ int sla_tree_mask_to_parent_host(const uint64_t *mask, int32_t n_nodes, int32_t 
  * cache_len[b] < 0, cache_len[b] + n_nodes > max_pages page_size or
  * cache_len[b] > max_len; SLA_ERR_PAGE if a page it needs is not in
  * [0, n_pages).  Its cache is then untouched and its outputs are unspecified;
- * no memory outside the given buffers is accessed. */
+ * no memory outside the given buffers is accessed.
+ *
+ * What a call writes (outputs, the pools it stores to, workspace, new_len,
+ * status) may overlap neither another of these nor what it reads, else
+ * SLA_ERR_ALIAS: cache_len too is read throughout a call, so new_len is a
+ * buffer of its own.  Pointers are 16-byte aligned but for int32 arrays, else
+ * SLA_ERR_UNSUPPORTED.  Results are the same from run to run.  The division of
+ * the keys over workgroups goes by the lengths of the whole batch, so the last
+ * bits of a sequence's outputs may differ from one batch to another. */
 typedef struct sla_attn_shape {
   int32_t batch;     /* B >= 1                                              */
   int32_t q_heads;   /* a multiple of kv_heads; query head h reads the kv
@@ -451,7 +459,7 @@ typedef struct sla_attn_transform {
  *     16 bytes.
  *   transform  norms and rotation; NULL: neither.
  *   parent_idx device int32 [B][n]; page_table [B][max_pages]; cache_len [B].
- *   q_out      device [B][n][q_heads][D]; must not overlap q, k or v.
+ *   q_out      device [B][n][q_heads][D].
  *   k_cache, v_cache  device [n_pages][kv_heads][page_size][D].
  *   status     device int32 [B] or NULL.
  * max_len is ignored. */
@@ -468,7 +476,8 @@ int sla_attn_append(const sla_attn_shape *shape, const sla_attn_transform *trans
  * included).  Scores, the softmax's running maximum and sum, and the outputs
  * are held in fp32; bf16 activations round the weights p to bf16 for the
  * matrix cores, fp32 ones are multiplied exactly.
- *   q, out  device [B][n][q_heads][D], activation dtype; they must not overlap.
+ *   scale   finite.
+ *   q, out  device [B][n][q_heads][D], activation dtype.
  *   k_cache, v_cache  device [n_pages][kv_heads][page_size][D].
  *   workspace  device memory of at least sla_attn_workspace_bytes(shape)
  *           bytes (may be NULL if that is 0), 16-byte aligned, used until the
@@ -490,8 +499,7 @@ size_t sla_attn_workspace_bytes(const sla_attn_shape *shape);
  *   parent_idx  the draft's parent array, device int32 [B][n].
  *   path, len   as in sla_pending: device int32 [B][n] (-1 padded) and [B].
  *   new_len     device int32 [B] or NULL: cache_len[b] + len[b] (cache_len[b]
- *               on an error).  It must not overlap cache_len, which the call
- *               reads throughout.
+ *               on an error).
  *   status      device int32 [B] or NULL (also SLA_ERR_PATH).
  * q_heads, topology and max_len are ignored. */
 int sla_attn_commit(const sla_attn_shape *shape, int32_t layers, void *k_cache, void *v_cache,

@@ -4,6 +4,8 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <cmath>
+
 #include "attn.hpp"
 #include "sla.h"
 
@@ -13,9 +15,36 @@ size_t act_bytes(int dtype) { return dtype == SLA_DTYPE_BF16 ? 2 : 4; }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-bool overlaps(const void *p, size_t pn, const void *q, size_t qn) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return a < b + qn && b < a + pn;
+struct Span {
+  const void *p;  // NULL: none
+  size_t bytes;
+};
+
+Span span_of(const void *p, size_t count, size_t size) { return Span{p, count * size}; }
+
+bool overlaps(const Span &x, const Span &y) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+  return x.p && y.p && a < b + y.bytes && b < a + x.bytes;
+}
+
+// Whether an output overlaps another one or a buffer the call reads.
+template <int W, int N>
+bool aliased(const Span (&writes)[W], const Span (&reads)[N]) {
+  for (int i = 0; i < W; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (overlaps(writes[i], writes[j])) return true;
+    for (int j = 0; j < N; ++j)
+      if (overlaps(writes[i], reads[j])) return true;
+  }
+  return false;
+}
+
+// A pool of `layers` layers; a size past any memory counts as 2^56 bytes.
+Span pool_span(const sla_attn_shape *s, int32_t layers, const void *p) {
+  const unsigned __int128 bytes = (unsigned __int128)layers * s->n_pages * s->kv_heads * s->page_size *
+                                  (unsigned)s->head_dim * act_bytes(s->qkv_dtype);
+  const unsigned __int128 most = (unsigned __int128)1 << 56;
+  return Span{p, (size_t)(bytes < most ? bytes : most)};
 }
 
 int hip_status(hipError_t e) { return e == hipSuccess ? SLA_OK : SLA_ERR_HIP; }
@@ -97,12 +126,19 @@ int sla_attn_append(const sla_attn_shape *shape, const sla_attn_transform *t, co
     if (t->rope_dim > 0 && t->rope_len < 1) return SLA_ERR_SHAPE;
     if (t->rope_dim > 0 && !t->rope) return SLA_ERR_NULL;
   }
-  const size_t nodes = (size_t)shape->batch * shape->n_nodes;
-  const size_t out_bytes = nodes * (size_t)qd * w;
-  if (overlaps(q_out, out_bytes, q, ((nodes - 1) * (size_t)q_stride + (size_t)qd) * w) ||
-      overlaps(q_out, out_bytes, k, ((nodes - 1) * (size_t)k_stride + (size_t)kd) * w) ||
-      overlaps(q_out, out_bytes, v, ((nodes - 1) * (size_t)v_stride + (size_t)kd) * w))
-    return SLA_ERR_ALIAS;
+  const size_t rows = (size_t)shape->batch, nodes = rows * shape->n_nodes;
+  const Span writes[] = {span_of(q_out, nodes * (size_t)qd, w), pool_span(shape, 1, k_cache),
+                         pool_span(shape, 1, v_cache), span_of(status, rows, 4)};
+  const Span reads[] = {span_of(q, (nodes - 1) * (size_t)q_stride + (size_t)qd, w),
+                        span_of(k, (nodes - 1) * (size_t)k_stride + (size_t)kd, w),
+                        span_of(v, (nodes - 1) * (size_t)v_stride + (size_t)kd, w),
+                        span_of(parent_idx, nodes, 4),
+                        span_of(page_table, rows * shape->max_pages, 4),
+                        span_of(cache_len, rows, 4),
+                        span_of(t ? t->q_norm : nullptr, D, 4),
+                        span_of(t ? t->k_norm : nullptr, D, 4),
+                        span_of(t && t->rope_dim ? t->rope : nullptr, t ? (size_t)t->rope_dim * t->rope_len : 0, 4)};
+  if (aliased(writes, reads)) return SLA_ERR_ALIAS;
   const int64_t step = 16 / (int64_t)w;  // elements of 16 bytes
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_cache) ||
       !aligned16(v_cache) || q_stride % step || k_stride % step || v_stride % step)
@@ -150,13 +186,18 @@ int sla_attn_verify(const sla_attn_shape *shape, float scale, const void *q, con
   const int st = check_shape(shape);
   if (st != SLA_OK) return st;
   if (!q || !k_cache || !v_cache || !parent_idx || !page_table || !cache_len || !out) return SLA_ERR_NULL;
+  if (!std::isfinite(scale)) return SLA_ERR_SHAPE;
   sla::AttnVerifyArgs a = verify_args(shape);
   const size_t need = sla::attn_workspace_bytes(a, shape->qkv_dtype);
   if (need && !workspace) return SLA_ERR_NULL;
   if (need && workspace_bytes < need) return SLA_ERR_SHAPE;
-  const size_t bytes = (size_t)shape->batch * shape->n_nodes * shape->q_heads * shape->head_dim * act_bytes(shape->qkv_dtype);
-  if (overlaps(q, bytes, out, bytes) || (need && (overlaps(workspace, need, out, bytes) || overlaps(workspace, need, q, bytes))))
-    return SLA_ERR_ALIAS;
+  const size_t rows = (size_t)shape->batch, nodes = rows * shape->n_nodes;
+  const size_t values = nodes * shape->q_heads * shape->head_dim, w = act_bytes(shape->qkv_dtype);
+  const Span writes[] = {span_of(out, values, w), span_of(need ? workspace : nullptr, need, 1), span_of(status, rows, 4)};
+  const Span reads[] = {span_of(q, values, w), pool_span(shape, 1, k_cache), pool_span(shape, 1, v_cache),
+                        span_of(parent_idx, nodes, 4), span_of(page_table, rows * shape->max_pages, 4),
+                        span_of(cache_len, rows, 4)};
+  if (aliased(writes, reads)) return SLA_ERR_ALIAS;
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace))
     return SLA_ERR_UNSUPPORTED;
   a.cache.k = const_cast<void *>(k_cache);
@@ -178,8 +219,12 @@ int sla_attn_commit(const sla_attn_shape *shape, int32_t layers, void *k_cache, 
   if (st != SLA_OK) return st;
   if (!layers_ok(shape, layers)) return SLA_ERR_SHAPE;
   if (!k_cache || !v_cache || !parent_idx || !path || !len || !page_table || !cache_len) return SLA_ERR_NULL;
-  const size_t row = (size_t)shape->batch * sizeof(int32_t);
-  if (new_len && (overlaps(new_len, row, cache_len, row) || overlaps(new_len, row, len, row))) return SLA_ERR_ALIAS;
+  const size_t rows = (size_t)shape->batch, nodes = rows * shape->n_nodes;
+  const Span writes[] = {pool_span(shape, layers, k_cache), pool_span(shape, layers, v_cache), span_of(new_len, rows, 4),
+                         span_of(status, rows, 4)};
+  const Span reads[] = {span_of(parent_idx, nodes, 4), span_of(path, nodes, 4), span_of(len, rows, 4),
+                        span_of(page_table, rows * shape->max_pages, 4), span_of(cache_len, rows, 4)};
+  if (aliased(writes, reads)) return SLA_ERR_ALIAS;
   if (!aligned16(k_cache) || !aligned16(v_cache)) return SLA_ERR_UNSUPPORTED;
   sla::AttnCommitArgs a;
   memset(&a, 0, sizeof(a));
@@ -202,6 +247,9 @@ int sla_page_copy(const sla_attn_shape *shape, int32_t layers, void *k_cache, vo
   if (st != SLA_OK) return st;
   if (!layers_ok(shape, layers) || copies < 1 || copies > (1 << 24)) return SLA_ERR_SHAPE;
   if (!k_cache || !v_cache || !src || !dst) return SLA_ERR_NULL;
+  const Span writes[] = {pool_span(shape, layers, k_cache), pool_span(shape, layers, v_cache), span_of(status, copies, 4)};
+  const Span reads[] = {span_of(src, copies, 4), span_of(dst, copies, 4), span_of(rows, copies, 4)};
+  if (aliased(writes, reads)) return SLA_ERR_ALIAS;
   if (!aligned16(k_cache) || !aligned16(v_cache)) return SLA_ERR_UNSUPPORTED;
   sla::PageCopyArgs a;
   memset(&a, 0, sizeof(a));

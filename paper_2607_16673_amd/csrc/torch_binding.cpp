@@ -341,6 +341,8 @@ Rows cache_rows(sla_attn_shape &s, PyObject *parent, PyObject *table, PyObject *
   const at::Tensor &p = sized(parent, 2, "parent_idx");
   const at::Tensor &t = sized(table, 2, "page_table");
   const int64_t B = p.size(0), n = p.size(1), pages = t.size(1);
+  TORCH_CHECK_VALUE(B <= INT32_MAX && n <= INT32_MAX && pages <= INT32_MAX, "parent_idx and page_table have shapes ",
+                    p.sizes(), " and ", t.sizes(), ", too large");
   s.batch = (int32_t)B;
   s.n_nodes = (int32_t)n;
   s.max_pages = (int32_t)pages;
@@ -380,6 +382,7 @@ PyObject *attn_append(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
   const int64_t B = c.shape.batch, n = c.shape.n_nodes, D = c.shape.head_dim, kh = c.shape.kv_heads;
   const at::Tensor &q = sized(o[0], 4, "q");
   const int64_t qh = q.size(2);
+  TORCH_CHECK_VALUE(qh <= INT32_MAX, "q has shape ", q.sizes(), ", too large");
   c.shape.q_heads = (int32_t)qh;
   c.shape.topology = (int32_t)number(o[15]);
   int64_t qs, ks, vs;
@@ -412,6 +415,7 @@ PyObject *attn_append(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
 // q [B][n][q heads][D] of a verification over this pool
 const void *queries(Pool &c, PyObject *qo, PyObject *max_len) {
   const at::Tensor &q = sized(qo, 4, "q");
+  TORCH_CHECK_VALUE(q.size(2) <= INT32_MAX, "q has shape ", q.sizes(), ", too large");
   c.shape.q_heads = (int32_t)q.size(2);
   c.shape.max_len = number32(max_len, "max_len");
   const int64_t B = c.shape.batch, n = c.shape.n_nodes, D = c.shape.head_dim;
@@ -449,10 +453,10 @@ PyObject *attn_workspace_bytes(PyObject *, PyObject *const *o, Py_ssize_t nargs)
   HANDLE_TH_ERRORS
   count_args(nargs, 6);
   Pool c = pool(o[3], o[3], false);
-  c.shape.batch = (int32_t)number(o[0]);
-  c.shape.n_nodes = (int32_t)number(o[1]);
-  c.shape.q_heads = (int32_t)number(o[2]);
-  c.shape.max_pages = (int32_t)number(o[4]);
+  c.shape.batch = number32(o[0], "batch");
+  c.shape.n_nodes = number32(o[1], "n_nodes");
+  c.shape.q_heads = number32(o[2], "q_heads");
+  c.shape.max_pages = number32(o[4], "max_pages");
   c.shape.max_len = number32(o[5], "max_len");
   return PyLong_FromSize_t(sla_attn_workspace_bytes(&c.shape));
   END_HANDLE_TH_ERRORS
