@@ -2,6 +2,7 @@
 
 The compute lives in ``libsla.so`` (hand-written HIP for gfx950 behind a
 C ABI, declared in ``include/sla.h``); ``binding`` marshals torch tensors
-into it.  ``inputs`` is the seeded synthetic workload generator.
+into it.  ``cache`` keeps the pages of the attention layers' cache and makes
+rotation tables; ``inputs`` is the seeded synthetic workload generator.
 """
-__all__ = ["binding", "inputs"]
+__all__ = ["binding", "cache", "inputs"]
