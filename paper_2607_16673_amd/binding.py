@@ -393,8 +393,6 @@ def sla_attn_verify(q, k_cache, v_cache, parent_idx, page_table, cache_len, out,
     q, out [B][n][Hq][D]; k_cache, v_cache [pages][Hkv][page size][D] with the
     draft appended; scale defaults to D^-0.5; max_len promises cache_len <=
     max_len (0: the page table's capacity); workspace: from attn_workspace."""
-    if scale is None:
-        scale = q.shape[-1] ** -0.5
     code = (_nat or native()).attn_verify(q, k_cache, v_cache, parent_idx, page_table, cache_len, out, scale, max_len,
                                           workspace, status, TOPOLOGIES[topology])
     _check(code, "sla_attn_verify")

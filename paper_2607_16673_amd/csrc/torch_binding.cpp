@@ -17,6 +17,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <initializer_list>
 
 #include "sla.h"
@@ -422,7 +423,7 @@ const void *queries(Pool &c, PyObject *qo, PyObject *max_len) {
   return device_pointer(q, c.tensor->scalar_type(), {B, n, q.size(2), D}, "q");
 }
 
-// attn_verify(q, k_cache, v_cache, parent_idx, page_table, cache_len, out, scale, max_len, workspace, status, topology)
+// attn_verify(q, k_cache, v_cache, parent_idx, page_table, cache_len, out, scale | None, max_len, workspace, status, topology)
 PyObject *attn_verify(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   count_args(nargs, 12);
@@ -432,7 +433,7 @@ PyObject *attn_verify(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
   c.shape.topology = (int32_t)number(o[11]);
   const int64_t B = c.shape.batch, n = c.shape.n_nodes, D = c.shape.head_dim;
   void *out = pointer(o[6], c.tensor->scalar_type(), {B, n, (int64_t)c.shape.q_heads, D}, "out");
-  const double scale = PyFloat_AsDouble(o[7]);
+  const double scale = o[7] == Py_None ? 1.0 / std::sqrt((double)D) : PyFloat_AsDouble(o[7]);
   if (scale == -1.0 && PyErr_Occurred()) throw python_error();
   void *ws = nullptr;
   size_t bytes = 0;
