@@ -3,7 +3,11 @@
 // q_out, keys and values to the paged cache.
 //
 // One pass: every element is read once and written once, so memory bounds it
-// for large drafts and the launch for small ones.  A head is the work of
+// for large drafts (256 sequences of 64 nodes of 16 + 2 + 2 fp32 heads of 256:
+// 132 us, 5.1 TB/s, the rate of a large copy) and the launch with its chain of loads
+// (length, page, rotation) for small ones (64 of
+// 16 nodes of heads of 128 in bf16: 5.6 us).  Norms,
+// angles and products are fp32, rounded once at the end.  A head is the work of
 // D / 8 neighbouring lanes, 8 elements (16 bytes of bf16) each: the mean
 // square is a butterfly over those lanes, and the partner of a rotated pair is
 // in the same lane (interleaved pairs) or rope_dim / 16 lanes away (halves).
