@@ -216,7 +216,9 @@ __device__ __forceinline__ bool pick_range(const AttnVerifyArgs &a, const Split 
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) sum += sum_s[0][w] + ((unsigned long long)sum_s[1][w] << 16);
   int most[kTries], count[kTries] = {};
-  const int hi = (int)((sum + s.share - 1) / s.share), lo = s.fine ? (int)((sum + s.parts - 1) / s.parts) : hi;
+  // (2^30 tiles are more than a sequence has: with them each has one range)
+  const int hi = (int)min((sum + s.share - 1) / s.share, 1ull << 30);
+  const int lo = s.fine ? (int)((sum + s.parts - 1) / s.parts) : hi;
 #pragma unroll
   for (int i = 0; i < kTries; ++i) most[i] = max(lo + (int)((long long)(hi - lo) * i / (kTries - 1)), 1);
   for (int b = b0; b < b1; ++b) {
