@@ -887,7 +887,10 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
       x += w * part_x[slot + k][e / 4];
     }
   }
-  if (a.status && i < rows && kv == 0 && r == 0) {  // (the row's lanes together)
+  if (a.status && i < rows && kv == 0 && r == 0) {
+    // the sequence's first row tells of it: its kLanes lanes alone, for a wave
+    // holds the first rows of several sequences where these have few
+    const uint64_t lanes = (~0ull >> (kWave - kLanes)) << (threadIdx.x % kWave / kLanes * kLanes);
     bool topology = false, page = false, length = false;
     for (int s = e / 4; s < own.y; s += kLanes) {
       const int err = split_errors(a, split, R)[own.x + s];
@@ -895,9 +898,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
       length |= err == SLA_ERR_LENGTH;
       page |= err == SLA_ERR_PAGE;
     }
-    topology = wave_any(topology);
-    length = wave_any(length);
-    page = wave_any(page);
+    topology = __ballot(topology) & lanes;
+    length = __ballot(length) & lanes;
+    page = __ballot(page) & lanes;
     if (e == 0) a.status[b] = topology ? SLA_ERR_TOPOLOGY : length ? SLA_ERR_LENGTH : page ? SLA_ERR_PAGE : SLA_OK;
   }
   if (!live) return;
