@@ -476,7 +476,7 @@ int sla_attn_append(const sla_attn_shape *shape, const sla_attn_transform *trans
  * included).  Scores, the softmax's running maximum and sum, and the outputs
  * are held in fp32; bf16 activations round the weights p to bf16 for the
  * matrix cores, fp32 ones are multiplied exactly.
- *   scale   finite.
+ *   scale   finite; 0 weighs all the rows of a node alike.
  *   q, out  device [B][n][q_heads][D], activation dtype.
  *   k_cache, v_cache  device [n_pages][kv_heads][page_size][D].
  *   workspace  device memory of at least sla_attn_workspace_bytes(shape)

@@ -339,6 +339,24 @@ __device__ __forceinline__ uint32_t own_offset(uint32_t x) {
   return x;
 }
 
+// -x; and 0 times x: zeros, and NaN where x is infinite or NaN.  (Opaque, so that a
+// branch around them stays one.)
+__device__ __forceinline__ bf16x8 minus(bf16x8 x) {
+  u32x4 y = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = own_offset(y[i]) ^ 0x80008000u;
+  return __builtin_bit_cast(bf16x8, y);
+}
+__device__ __forceinline__ bf16x8 zero_times(bf16x8 x) {
+  u32x4 y = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = own_offset(y[i]);
+    y[i] = ((w & 0x7f80u) == 0x7f80u ? 0x7fc0u : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0x7fc00000u : 0u);
+  }
+  return __builtin_bit_cast(bf16x8, y);
+}
+
 // Where the piece at `offset` of a row lies for a lane whose swizzle is `lane`
 // (below 256): a few exclusive-ors for a row, the rest in the reads' immediates.
 __device__ __forceinline__ int place(int offset, int lane) { return (offset % 256 ^ lane) + offset / 256 * 256; }
@@ -448,6 +466,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
     // this wave's queries
     const int r0 = qt0 + wave / WK * (QT * kQueries), wk = wave % WK;
     const bool active = r0 < R;
+    const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f;
     Frag<T, D> qf[QT];
     int node[QT];
 #pragma unroll
@@ -457,16 +476,12 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
       const T *q = static_cast<const T *>(a.q) + (((size_t)b * n + r / G) * a.Hq + (size_t)kv * G + r % G) * D;
       if constexpr (L::kBf16) {
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          u32x4 x = *reinterpret_cast<const u32x4 *>(q + 32 * c + 8 * g);
-          if (a.scale < 0.f) x ^= 0x80008000u;
-          qf[t].x[c] = __builtin_bit_cast(bf16x8, x);
-        }
+        for (int c = 0; c < D / 32; ++c) qf[t].x[c] = *reinterpret_cast<const bf16x8 *>(q + 32 * c + 8 * g);
       } else {
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
           const f32x4 x = *reinterpret_cast<const f32x4 *>(q + 16 * c + 4 * g);
-          qf[t].x[c] = a.scale < 0.f ? -x : x;
+          qf[t].x[c] = x * sign;
         }
       }
     }
@@ -480,9 +495,9 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    // weights are powers of two; the scale's sign is in the queries, and a scale
-    // of 0 is one too small to part any scores, so that masked ones stay -inf
-    const float scale = fmaxf(fabsf(a.scale) * 1.44269504088896341f, 1e-30f);
+    // Weights are powers of two; the scale's sign is in the queries, and so is a
+    // scale of 0: times 0, masked scores would not stay -inf.
+    const float scale = sign == 0.f ? 1.f : fabsf(a.scale) * 1.44269504088896341f;
 
     // fragment reads: this lane's row of a key tile, and the pieces' places in it
     const int k_row = (wk * kKeyTiles * 16 + col) * L::kRow;
@@ -677,6 +692,15 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
     // (64 sequences of 16-node trees 50.7 -> 48.7 us).  Workgroups numbered 256
     // apart usually meet.
     if (WAVES == 4 && (blockIdx.x >> 8) & 1) __builtin_amdgcn_s_setprio(2);
+    if constexpr (L::kBf16) {
+      // (here, where nothing waits for them yet: as they are read, one token takes 9.23 us, not 9.00)
+      if (!(sign > 0.f)) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (auto &x : qf[t].x) x = sign < 0.f ? minus(x) : zero_times(x);
+      }
+    }
     int buf = 0;
     for (int k0 = k_begin; k0 < k_end; k0 += L::kKeys, buf ^= 1) {
       __syncthreads();  // the tile is whole, and the other buffer free
