@@ -78,11 +78,25 @@ struct Tile {
 // workgroup has more to do than another, but a sequence's start costs some of
 // them a second time what it costs to begin.  share and workers 0: a workgroup a
 // sequence, and no workspace.
+//
+// The workspace has room for the parts of divided sequences alone, `slots` of
+// them; a sequence that one workgroup has to itself goes straight to the output.
+//   Ranges, fine: one each.
+//   Ranges, by `share`: a divided sequence of t tiles in ranges of m < t has fewer
+//   than 2 t / m of them, and all tiles over m are at most `share`: 2 share.
+//   Equal parts: a worker may go on with one sequence that another began, the slot
+//   of its number, and begin one that another goes on with, a slot behind those by
+//   the sequence's number or, if there are fewer of them, by the worker's.
 struct Split {
   int share, parts;
   bool fine;  // as many ranges as `parts` allows, rather than as few as `share` asks for
   int workers;
+  int slots;
   __host__ __device__ bool divided() const { return share > 0 || workers > 0; }
+  // the first part of sequence b, whose first range or worker is `first`
+  __host__ __device__ int first_slot(int first, int b, int B) const {
+    return workers == 0 ? first : workers + (B <= workers ? b : first);
+  }
 };
 
 // A query fragment: the B operand of S^T = K Q^T for 16 queries.
@@ -125,11 +139,11 @@ __device__ __forceinline__ f32x4 load4(const bf16 *p) {
 }
 __device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
 
-// The workspace of a split launch: unnormalised outputs [Hkv][parts][R][D],
-// their reference and sum [Hkv][parts][R], each sequence's first part and how
-// many it has [B], each part's error [parts].
+// The workspace of a split launch: unnormalised outputs [Hkv][slots][R][D],
+// their reference and sum [Hkv][slots][R], each sequence's first part (the number
+// of its range or worker) and how many it has [B], each part's error [slots].
 __host__ __device__ inline size_t split_rows(const AttnVerifyArgs &a, const Split &s, int R) {
-  return (size_t)a.cache.Hkv * s.parts * R;
+  return (size_t)a.cache.Hkv * s.slots * R;
 }
 __device__ __forceinline__ float2 *split_stats(const AttnVerifyArgs &a, const Split &s, int R) {
   return reinterpret_cast<float2 *>(static_cast<float *>(a.workspace) + split_rows(a, s, R) * a.cache.D);
@@ -170,7 +184,7 @@ __device__ __forceinline__ int tiles_of(const AttnVerifyArgs &a, int len) {
 }
 
 struct Range {
-  int b, part, parts, first;  // the sequence, which of its ranges, how many, the number of the first
+  int b, part, parts, first;  // the sequence, which of its ranges, how many, the slot of the first
 };
 
 // The range number `item` of a launch: false if there are fewer.  All threads
@@ -182,7 +196,7 @@ template <int KEYS, int WAVES>
 __device__ __forceinline__ bool pick_range(const AttnVerifyArgs &a, const Split &s, int item, Range &r) {
   constexpr int kTries = 4;
   __shared__ uint32_t sum_s[2][WAVES];
-  __shared__ int count_s[kTries][WAVES], scan_s[WAVES];
+  __shared__ int count_s[kTries][WAVES], scan_s[2][WAVES];
   __shared__ Range found_s;
   auto tiles_of = [&](int b) { return sla::tiles_of<KEYS>(a, a.rows.len[b]); };
   auto over = [](int tiles, int most) { return (tiles + most - 1) / most; };
@@ -221,10 +235,12 @@ __device__ __forceinline__ bool pick_range(const AttnVerifyArgs &a, const Split 
   const int lo = s.fine ? (int)((sum + s.parts - 1) / s.parts) : hi;
 #pragma unroll
   for (int i = 0; i < kTries; ++i) most[i] = max(lo + (int)((long long)(hi - lo) * i / (kTries - 1)), 1);
+  int divided = 0;  // ranges of this thread's divided sequences, by `share`
   for (int b = b0; b < b1; ++b) {
     const int t = tiles_of(b);
 #pragma unroll
     for (int i = 0; i < kTries; ++i) count[i] += over(t, most[i]);
+    if (!s.fine && t > hi) divided += over(t, hi);
   }
 #pragma unroll
   for (int i = 0; i < kTries; ++i) {
@@ -247,21 +263,30 @@ __device__ __forceinline__ bool pick_range(const AttnVerifyArgs &a, const Split 
     }
   }
   if (item >= all) return false;
-  int before = wave_scan(mine);  // ranges of this thread's sequences and of those in front of them
-  if (lane == kWave - 1) scan_s[wave] = before;
+  // ranges of this thread's sequences and of those in front of them; and slots
+  int before = wave_scan(mine), slot = wave_scan(divided);
+  if (lane == kWave - 1) {
+    scan_s[0][wave] = before;
+    scan_s[1][wave] = slot;
+  }
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < WAVES; ++w)
-    if (w < wave) before += scan_s[w];
+    if (w < wave) {
+      before += scan_s[0][w];
+      slot += scan_s[1][w];
+    }
   int first = before - mine;
+  slot -= divided;
   if (item >= first && item < before)
     for (int b = b0; b < b1; ++b) {
       const int parts = over(tiles_of(b), longest);
       if (item < first + parts) {
-        found_s = Range{b, item - first, parts, first};
+        found_s = Range{b, item - first, parts, s.fine ? first : slot};
         break;
       }
       first += parts;
+      if (parts > 1) slot += parts;
     }
   __syncthreads();
   r = found_s;
@@ -400,16 +425,18 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
   const bool reports = kv == 0 && qt0 == 0;  // this workgroup tells of its parts and their errors
   const int shift = a.cache.page_shift;
   const const_int *const lens = (const const_int *)(uintptr_t)a.rows.len;
-  // sequence b's tiles from..to of `tiles`
-  auto attend = [&](const int b, const int len, const int tiles, const int from, const int to, const int slot,
-                    auto parts_of) __attribute__((always_inline)) {
+  // sequence b's tiles from..to of `tiles`; its first part is number `first`, this
+  // one's slot `slot` if the sequence is divided
+  auto attend = [&](const int b, const int len, const int tiles, const int from, const int to, const int first,
+                    const int slot, auto parts_of) __attribute__((always_inline)) {
     // (opaque where registers are short: what is formed from it is formed again
     // for the next sequence, or next to its use, and not kept)
     const int tid = SPAN || QT * D >= 512 ? own_offset(threadIdx.x) : threadIdx.x, lane = tid % kWave;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int g = lane / 16, col = lane % 16;
-    int32_t *const err = split.divided() ? split_errors(a, split, R) + slot : a.status ? a.status + b : nullptr;
-    if (reports && split.divided() && from == 0 && tid == 0) split_parts(a, split, R)[b] = make_int2(slot, parts_of());
+    const bool whole = from == 0 && to == tiles;  // no other workgroup has keys of these rows
+    int32_t *const err = !whole ? split_errors(a, split, R) + slot : a.status ? a.status + b : nullptr;
+    if (reports && split.divided() && from == 0 && tid == 0) split_parts(a, split, R)[b] = make_int2(first, parts_of());
     if (!length_ok(a.rows, shift, len, n) || len > a.max_len) {
       if (reports && err && tid == 0) *err = SLA_ERR_LENGTH;
       return;
@@ -777,7 +804,6 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
       }
     }
 
-    const bool whole = from == 0 && to == tiles;  // no other workgroup has keys of these rows
     float *const ws = static_cast<float *>(a.workspace);
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -795,7 +821,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
             *reinterpret_cast<f32x4 *>(out + d * 16) = x;
         }
       } else {
-        const size_t row = ((size_t)kv * split.parts + slot) * R + r;
+        const size_t row = ((size_t)kv * split.slots + slot) * R + r;
         float *out = ws + row * D + 4 * g;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4 *>(out + d * 16) = o[t][d];
@@ -809,8 +835,9 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
     if (!pick_range<L::kKeys, WAVES>(a, split, item, range)) return;
     const int b = __builtin_amdgcn_readfirstlane(range.b), parts = __builtin_amdgcn_readfirstlane(range.parts);
     const int part = __builtin_amdgcn_readfirstlane(range.part), len = lens[b], tiles = tiles_of<L::kKeys>(a, len);
-    attend(b, len, tiles, (int)((int64_t)tiles * part / parts), (int)((int64_t)tiles * (part + 1) / parts),
-           __builtin_amdgcn_readfirstlane(range.first) + part, [&] { return parts; });
+    const int first = __builtin_amdgcn_readfirstlane(range.first);
+    attend(b, len, tiles, (int)((int64_t)tiles * part / parts), (int)((int64_t)tiles * (part + 1) / parts), first,
+           first + part, [&] { return parts; });
   } else {
     // This worker's part [begin, end) of the tiles of all sequences: the first
     // `more` workers have one more than `each`.
@@ -831,7 +858,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
       const int to = end < before + tiles ? (int)(end - before) : tiles;  // not above 0 if the part ends in the start's share
       const int next = lens[min(b + 1, a.B - 1)];
       if (from < to)
-        attend(b, len, tiles, from, to, item + b, [&] {  // up to the worker that has the sequence's last tile
+        attend(b, len, tiles, from, to, item, from > 0 ? item : split.first_slot(item, b, a.B), [&] {
+          // up to the worker that has the sequence's last tile
           const uint64_t last = before + tiles - 1, longer = (each + 1) * more;
           return 1 - item + (int)(last < longer ? quotient(last, (uint32_t)each + 1)
                                                 : more + quotient(last - longer, (uint32_t)each));
@@ -863,8 +891,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
   const int r = i % R, kv = i / R % Hkv, b = min((int)(i / R / Hkv), a.B - 1);
   const int2 own = split_parts(a, split, R)[b];
   const bool live = i < rows && own.y > 1;  // else written whole
-  const int parts = live ? own.y : 0;
-  const size_t row0 = ((size_t)kv * split.parts + own.x) * R + r;
+  const int parts = live ? own.y : 0, slot0 = split.first_slot(own.x, b, a.B);
+  auto slot_of = [&](int s) { return s > 0 ? own.x + s : slot0; };
+  const size_t row0 = (size_t)kv * split.slots * R + r;
   const float *const ws = static_cast<const float *>(a.workspace) + row0 * D + e;
   const float2 *const ml = split_stats(a, split, R) + row0;
   float ref = kNoScore, l = 0.f;
@@ -874,7 +903,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
     f32x4 y[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      const size_t s = min(s0 + k * GROUPS, parts - 1);
+      const size_t s = slot_of(min(s0 + k * GROUPS, parts - 1));
       st[k] = ml[s * R];
       y[k] = *reinterpret_cast<const f32x4 *>(ws + s * R * D);
     }
@@ -911,13 +940,13 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
       x += w * part_x[slot + k][e / 4];
     }
   }
-  if (a.status && i < rows && kv == 0 && r == 0) {
+  if (a.status && live && kv == 0 && r == 0) {
     // the sequence's first row tells of it: its kLanes lanes alone, for a wave
     // holds the first rows of several sequences where these have few
     const uint64_t lanes = (~0ull >> (kWave - kLanes)) << (threadIdx.x % kWave / kLanes * kLanes);
     bool topology = false, page = false, length = false;
     for (int s = e / 4; s < own.y; s += kLanes) {
-      const int err = split_errors(a, split, R)[own.x + s];
+      const int err = split_errors(a, split, R)[slot_of(s)];
       topology |= err == SLA_ERR_TOPOLOGY;
       length |= err == SLA_ERR_LENGTH;
       page |= err == SLA_ERR_PAGE;
@@ -986,7 +1015,7 @@ Split plan(const AttnVerifyArgs &a) {
   const int R = a.n * (a.Hq / a.cache.Hkv);
   const Form f = form_of<T, D>(R);
   const int64_t tiles = ((int64_t)a.max_len + a.n + kKeys - 1) / kKeys;  // of the longest sequence there may be
-  if (tiles == 1) return Split{0, a.B, false, 0};
+  if (tiles == 1) return Split{0, a.B, false, 0, 0};
   // workgroups that run at once, and the ranges that makes of the batch's keys
   const int64_t slots = (int64_t)device_cus() * (8 / f.waves);
   const int64_t want = std::max<int64_t>(1, slots / ((int64_t)a.cache.Hkv * ((R + f.rows() - 1) / f.rows())));
@@ -995,12 +1024,15 @@ Split plan(const AttnVerifyArgs &a) {
   // start of a second sequence costs short work more than it saves, 64 of up to
   // 4096 and 16-node trees 49 -> 52 us.
   if (a.B > 1 && want >= kFewWorkers && a.B * tiles >= kLongWork * want)
-    return Split{0, (int)(want + a.B - 1), false, (int)want};
+    return Split{0, (int)(want + a.B - 1), false, (int)want, (int)(want + std::min<int64_t>(want, a.B))};
   for (int64_t ranges = want; ranges <= 2 * want; ranges += want)
-    if (ranges > a.B) return Split{(int)(ranges - a.B), (int)std::min<int64_t>(ranges, a.B * tiles), true, 0};
+    if (ranges > a.B) {
+      const int parts = (int)std::min<int64_t>(ranges, a.B * tiles);
+      return Split{(int)(ranges - a.B), parts, true, 0, parts};
+    }
   // more sequences than that: only one much longer than a workgroup's even share is divided
   const int64_t share = (want + 1) / 2;
-  return Split{(int)std::max<int64_t>(share, 1), (int)std::min<int64_t>(share + 1 + a.B, a.B * tiles), false, 0};
+  return Split{(int)share, (int)std::min<int64_t>(share + 1 + a.B, a.B * tiles), false, 0, (int)(2 * share)};
 }
 
 template <typename T, int D, int QT, int WK, int WAVES>
@@ -1073,7 +1105,7 @@ size_t attn_workspace_bytes(const AttnVerifyArgs &a, int dtype) {
                                          : (bf ? plan<bf16, 256>(a) : plan<float, 256>(a));
   if (!split.divided()) return 0;
   return split_rows(a, split, a.n * (a.Hq / a.cache.Hkv)) * (a.cache.D + 2) * sizeof(float) +
-         (size_t)a.B * sizeof(int2) + (size_t)split.parts * sizeof(int32_t);
+         (size_t)a.B * sizeof(int2) + (size_t)split.slots * sizeof(int32_t);
 }
 
 hipError_t launch_attn_verify(const AttnVerifyArgs &a, int dtype, hipStream_t s) {
