@@ -411,7 +411,8 @@ int sla_tree_mask_to_parent_host(const uint64_t *mask, int32_t n_nodes, int32_t 
 typedef struct sla_attn_shape {
   int32_t batch;     /* B >= 1                                              */
   int32_t q_heads;   /* a multiple of kv_heads; query head h reads the kv
-                        head h / (q_heads / kv_heads)                       */
+                        head h / (q_heads / kv_heads); batch n_nodes q_heads
+                        < 2^31                                              */
   int32_t kv_heads;  /* >= 1                                                */
   int32_t head_dim;  /* D: 64, 128 or 256                                   */
   int32_t n_nodes;   /* draft nodes per sequence, 1..SLA_MAX_NODES          */

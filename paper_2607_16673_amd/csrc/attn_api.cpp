@@ -79,11 +79,13 @@ int check_shape(const sla_attn_shape *s) {
   if (st != SLA_OK) return st;
   if (s->q_heads < 1 || s->q_heads % s->kv_heads || s->q_heads > (1 << 16) || s->max_len < 0) return SLA_ERR_SHAPE;
   if (s->topology != SLA_TOPO_TREE && s->topology != SLA_TOPO_CHAIN) return SLA_ERR_SHAPE;
+  // the rows' numbers, and those of a launch's workgroups, which are not many more, fit 32 bits
+  if ((int64_t)s->batch * s->n_nodes * s->q_heads >= (1ll << 31)) return SLA_ERR_SHAPE;
   return SLA_OK;
 }
 
 bool layers_ok(const sla_attn_shape *s, int32_t layers) {
-  // grid sizes stay far inside 2^31 workgroups
+  // a launch's first dimension stays far inside 2^32 work-items
   return layers >= 1 && layers <= (1 << 16) && (int64_t)layers * s->kv_heads <= (1 << 20);
 }
 

@@ -85,24 +85,27 @@ hipError_t launch_commit_c(const AttnCommitArgs &a, hipStream_t s) {
 }
 
 // Copy.  One workgroup: the rows of one page in one head of one layer's keys
-// or values, which are contiguous.
+// or values, which are contiguous; of more than one page if there are more copies
+// than a launch is high.
+constexpr int kGridHeight = 65535;
+
 __global__ __launch_bounds__(kThreads) void page_copy_kernel(PageCopyArgs a, int cols) {
   const int Hkv = a.cache.Hkv, shift = a.cache.page_shift;
-  const int pieces = a.layers * 2 * Hkv;
-  const unsigned i = blockIdx.x / pieces;
-  const int piece = blockIdx.x % pieces;
-  const int src = a.src[i], dst = a.dst[i], rows = a.rows ? a.rows[i] : 1 << shift;
-  int err = SLA_OK;
-  if (src < 0 || src >= a.cache.n_pages || dst < 0 || dst >= a.cache.n_pages) err = SLA_ERR_PAGE;
-  else if (rows < 0 || rows > 1 << shift) err = SLA_ERR_LENGTH;
-  if (a.status && piece == 0 && threadIdx.x == 0) a.status[i] = err;
-  if (err != SLA_OK || src == dst) return;
+  const int piece = blockIdx.x;
   const int h = piece % Hkv, kv = piece / Hkv % 2, layer = piece / Hkv / 2;
   uint4 *base = static_cast<uint4 *>(kv ? a.cache.v : a.cache.k) + (((size_t)layer * a.cache.n_pages * Hkv) << shift) * cols;
-  const uint4 *from = base + page_row(a.cache, src, h) * cols;
-  uint4 *to = base + page_row(a.cache, dst, h) * cols;
-  const int total = rows * cols;
-  for (int c = threadIdx.x; c < total; c += kThreads) to[c] = from[c];
+  for (int i = blockIdx.y; i < a.copies; i += kGridHeight) {
+    const int src = a.src[i], dst = a.dst[i], rows = a.rows ? a.rows[i] : 1 << shift;
+    int err = SLA_OK;
+    if (src < 0 || src >= a.cache.n_pages || dst < 0 || dst >= a.cache.n_pages) err = SLA_ERR_PAGE;
+    else if (rows < 0 || rows > 1 << shift) err = SLA_ERR_LENGTH;
+    if (a.status && piece == 0 && threadIdx.x == 0) a.status[i] = err;
+    if (err != SLA_OK || src == dst) continue;
+    const uint4 *from = base + page_row(a.cache, src, h) * cols;
+    uint4 *to = base + page_row(a.cache, dst, h) * cols;
+    const int total = rows * cols;
+    for (int c = threadIdx.x; c < total; c += kThreads) to[c] = from[c];
+  }
 }
 
 }  // namespace
@@ -118,9 +121,8 @@ hipError_t launch_attn_commit(const AttnCommitArgs &a, int dtype, hipStream_t s)
 
 hipError_t launch_page_copy(const PageCopyArgs &a, int dtype, hipStream_t s) {
   const int cols = a.cache.D * (dtype == SLA_DTYPE_BF16 ? 2 : 4) / 16;
-  const uint64_t blocks = (uint64_t)a.copies * a.layers * 2 * a.cache.Hkv;
-  if (blocks >= (1ull << 31)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(page_copy_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, cols);
+  const dim3 grid((unsigned)(a.layers * 2 * a.cache.Hkv), (unsigned)(a.copies < kGridHeight ? a.copies : kGridHeight));
+  hipLaunchKernelGGL(page_copy_kernel, grid, dim3(kThreads), 0, s, a, cols);
   return hipGetLastError();
 }
 

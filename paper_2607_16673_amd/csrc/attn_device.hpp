@@ -8,6 +8,16 @@
 
 namespace sla {
 
+// A launch's work-items are counted in 32 bits in each dimension, so large ones
+// go on in the second: workgroup `number` of up to 2^32.  The width is a multiple
+// of the XCDs and of 256.
+constexpr unsigned kGridWidth = 1u << 22;
+__device__ __forceinline__ unsigned workgroup() { return blockIdx.y * kGridWidth + blockIdx.x; }
+inline dim3 grid_of(uint64_t workgroups) {
+  if (workgroups <= kGridWidth) return dim3((unsigned)workgroups);
+  return dim3(kGridWidth, (unsigned)((workgroups + kGridWidth - 1) / kGridWidth));
+}
+
 // round to nearest even, two values to one word
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return (uint32_t)__builtin_bit_cast(uint16_t, static_cast<__bf16>(lo)) |

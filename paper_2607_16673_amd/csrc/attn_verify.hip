@@ -418,7 +418,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
   const int n = a.n, Hkv = a.cache.Hkv, G = a.Hq / Hkv, R = n * G;
   // the query tiles of one key range, which read the same keys, are numbered
   // back to back on one XCD
-  const unsigned turn = blockIdx.x / kXcdCount;
+  const unsigned turn = workgroup() / kXcdCount;
   unsigned u = turn / qtiles * kXcdCount + blockIdx.x % kXcdCount;
   const int qt0 = turn % qtiles * (WAVES / WK * QT * kQueries);
   const int kv = u % Hkv, item = u / Hkv;
@@ -887,7 +887,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split 
   const int n = a.n, Hkv = a.cache.Hkv, G = a.Hq / Hkv, R = n * G;
   const size_t rows = (size_t)a.B * Hkv * R;
   const int slot = threadIdx.x / kLanes, grp = slot % GROUPS, e = threadIdx.x % kLanes * 4;
-  const size_t i = (size_t)blockIdx.x * (kSlots / GROUPS) + slot / GROUPS;
+  const size_t i = (size_t)workgroup() * (kSlots / GROUPS) + slot / GROUPS;
   const int r = i % R, kv = i / R % Hkv, b = min((int)(i / R / Hkv), a.B - 1);
   const int2 own = split_parts(a, split, R)[b];
   const bool live = i < rows && own.y > 1;  // else written whole
@@ -1040,18 +1040,16 @@ hipError_t launch_form(const AttnVerifyArgs &a, const Form &f, const Split &spli
   const int R = a.n * (a.Hq / a.cache.Hkv), qtiles = (R + f.rows() - 1) / f.rows();
   const uint64_t items = (uint64_t)(split.workers ? split.workers : split.parts) * a.cache.Hkv;
   const uint64_t blocks = (items + kXcdCount - 1) / kXcdCount * kXcdCount * qtiles;
-  if (blocks >= (1ull << 31)) return hipErrorInvalidValue;
   auto *const kernel = split.workers ? verify_kernel<T, D, QT, WK, WAVES, true> : verify_kernel<T, D, QT, WK, WAVES, false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(WAVES * kWave), 0, s, a, split, qtiles);
+  hipLaunchKernelGGL(kernel, grid_of(blocks), dim3(WAVES * kWave), 0, s, a, split, qtiles);
   return hipGetLastError();
 }
 
 template <typename T, int D, int GROUPS>
 hipError_t launch_join(const AttnVerifyArgs &a, const Split &split, hipStream_t s) {
   constexpr int kRows = kThreads / (D / 4) / GROUPS;  // of a workgroup
-  const uint64_t rows = (uint64_t)a.B * a.n * a.Hq, blocks = (rows + kRows - 1) / kRows;
-  if (blocks >= (1ull << 31)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((join_kernel<T, D, GROUPS>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a, split);
+  const uint64_t rows = (uint64_t)a.B * a.n * a.Hq;
+  hipLaunchKernelGGL((join_kernel<T, D, GROUPS>), grid_of((rows + kRows - 1) / kRows), dim3(kThreads), 0, s, a, split);
   return hipGetLastError();
 }
 
