@@ -79,7 +79,7 @@ class Session:
     def verify(self, tokens, parent):
         """Logits [B][n][VOCAB] of every draft node; nothing is committed yet."""
         t, B, n = self.t, self.B, tokens.shape[1]
-        copies = [c for s in self.seqs for c in self.pool.reserve(s, n)]
+        copies = self.pool.reserve_all(self.seqs, n)
         if copies:  # pages that a fork shared until now
             src, dst, rows = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in zip(*copies))
             sla.sla_page_copy(*self.cache, src, dst, rows=rows)

@@ -7,7 +7,7 @@ rotation's table.
     ...                             # append, verify, commit with pool.table([a, ...])
     a.length += accepted
     b = pool.fork(a)                # shares a's pages until one of them writes
-    copies = pool.reserve(b, n)     # [(src, dst, rows)] for sla_page_copy
+    copies = pool.reserve_all([a, b], n)  # [(src, dst, rows)] for sla_page_copy
     pool.free(a)
 
 The pool only keeps numbers; the pages are the caller's tensors.
@@ -49,24 +49,41 @@ class PagePool:
         Returns the copies [(src, dst, rows)] that have to be made, in all layers,
         before those rows are written and before a page is freed.  Raises
         MemoryError, with nothing changed, if there are too few pages."""
+        return self.reserve_all([seq], rows)
+
+    def reserve_all(self, seqs, rows: int):
+        """`reserve` for every sequence of a batch, all or none of it: after a
+        MemoryError no sequence has changed.  (Of several calls of `reserve` the
+        copies of those before the error still have to be made.)"""
         if rows < 0:
             raise ValueError("rows must not be negative")
+        if len(set(seqs)) < len(seqs):
+            raise ValueError("a batch has each sequence once")
         if rows == 0:
             return []
         size = self.page_size
-        first, end = seq.length // size, -(-(seq.length + rows) // size)
-        shared = [i for i in range(first, min(end, len(seq.pages))) if self.holders[seq.pages[i]] > 1]
-        need = len(shared) + max(end - len(seq.pages), 0)
+        need, plan, left = 0, [], {}  # left: how often the batch's earlier sequences leave a page for a copy
+        for seq in seqs:
+            first, end = seq.length // size, -(-(seq.length + rows) // size)
+            shared = []
+            for i in range(first, min(end, len(seq.pages))):
+                p = seq.pages[i]
+                if self.holders[p] - left.get(p, 0) > 1:
+                    left[p] = left.get(p, 0) + 1
+                    shared.append(i)
+            need += len(shared) + max(end - len(seq.pages), 0)
+            plan.append((seq, first, end, shared))
         if need > len(self._free):
             raise MemoryError("%d pages needed, %d free" % (need, len(self._free)))
         copies = []
-        for i in shared:
-            src, seq.pages[i] = seq.pages[i], self._take()
-            self.holders[src] -= 1
-            if i == first and seq.length % size:
-                copies.append((src, seq.pages[i], seq.length % size))
-        while len(seq.pages) < end:
-            seq.pages.append(self._take())
+        for seq, first, end, shared in plan:
+            for i in shared:
+                src, seq.pages[i] = seq.pages[i], self._take()
+                self.holders[src] -= 1
+                if i == first and seq.length % size:
+                    copies.append((src, seq.pages[i], seq.length % size))
+            while len(seq.pages) < end:
+                seq.pages.append(self._take())
         return copies
 
     def fork(self, seq: Sequence) -> Sequence:
