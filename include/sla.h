@@ -373,15 +373,15 @@ int sla_tree_mask_to_parent_host(const uint64_t *mask, int32_t n_nodes, int32_t 
 
 /* ---------------------------------------- attention over a paged cache
  *
- * The hybrid models that SpecLA's targets belong to interleave their
- * recurrent layers with attention layers.  For one of these, a speculative
- * round is: the draft's keys and values enter the cache behind the committed
- * tokens (sla_attn_append, which also normalises and rotates queries and
- * keys), every node attends to the committed tokens and to its own root path
- * (sla_attn_verify), and the accepted path's rows move together behind the
- * committed tokens (sla_attn_commit).  A 1-node draft is the decode step.  A
- * prompt is a batch of 64-node chains that share one page-table row, the
- * chunk c with cache_len 64 c: append all of them, then verify all of them.
+ * Hybrid models interleave recurrent layers with attention layers.  For
+ * one of these, a speculative round is: the draft's keys and values enter
+ * the cache behind the committed tokens (sla_attn_append, which also
+ * normalises and rotates queries and keys), every node attends to the
+ * committed tokens and to its own root path (sla_attn_verify), and the
+ * accepted path's rows move together behind the committed tokens
+ * (sla_attn_commit).  A 1-node draft is the decode step.  A prompt is a
+ * batch of 64-node chains that share one page-table row, the chunk c with
+ * cache_len 64 c: append all of them, then verify all of them.
  *
  * Cache.  Keys and values lie in two pools of pages,
  *     [layers][n_pages][kv_heads][page_size][head_dim]
@@ -424,8 +424,9 @@ typedef struct sla_attn_shape {
   int32_t max_pages; /* entries of a page-table row; max_pages page_size
                         <= 2^30                                             */
   int32_t max_len;   /* promise that cache_len[b] <= max_len, by which
-                        sla_attn_verify lays out its work; 0: none, the
-                        page table's capacity                               */
+                        sla_attn_verify lays out its work (fastest when the
+                        longest sequence comes near it); 0: none, the page
+                        table's capacity                                    */
 } sla_attn_shape;
 
 #define SLA_ROPE_HALF 0        /* pairs (x[i], x[i + rope_dim / 2])          */
@@ -482,7 +483,9 @@ int sla_attn_append(const sla_attn_shape *shape, const sla_attn_transform *trans
  *   k_cache, v_cache  device [n_pages][kv_heads][page_size][D].
  *   workspace  device memory of at least sla_attn_workspace_bytes(shape)
  *           bytes (may be NULL if that is 0), 16-byte aligned, used until the
- *           call's work has finished; it needs no initialisation.
+ *           call's work has finished; it needs no initialisation.  It holds the
+ *           unfinished outputs of the workgroups that run at once, and 8 bytes a
+ *           sequence: beyond a filled chip it hardly grows with the batch.
  *   status  device int32 [B] or NULL. */
 int sla_attn_verify(const sla_attn_shape *shape, float scale, const void *q, const void *k_cache,
                     const void *v_cache, const int32_t *parent_idx, const int32_t *page_table,

@@ -12,10 +12,13 @@
 // statistics in the workspace, and a second kernel joins them.
 //
 // What bounds it: for one token or few rows the cache's bytes, 256 sequences of
-// up to 16384 keys 372 us, 5.8 TB/s; for many rows the matrix cores, 64-node
-// trees over up to 8192 keys with heads of 256 450 us, 780 TFLOP/s; for short
-// work the chain of loads that a workgroup starts with (length, page, rows) and
-// the second launch, one token over 1000 keys 9.9 us.
+// up to 16384 keys 372 us, 5.8 TB/s.  For many rows no one unit: the waves of a
+// SIMD wait for one another between products, exponentials and fragment reads.
+// 64-node trees over up to 8192 keys with heads of 256 take 424 us, 830 TFLOP/s,
+// the matrix cores busy 44% of the time and the LDS 27%; a 32-node tree over
+// 131072 keys 54.8 us, 37% and 23%.  For short work it is the chain of loads that a
+// workgroup starts with (length, page, rows) and the second launch, one token over
+// 1000 keys 9.1 us.  (States in turn, the card warm.)
 //
 // On the matrix cores the scores are formed transposed, S^T = K Q^T: a lane
 // of v_mfma_f32_16x16x32_bf16 then holds four consecutive keys of one query,
@@ -716,8 +719,10 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
     if (k_begin + L::kKeys < k_end) read_rows(k_begin + L::kKeys, true, kTogether);
     // Two workgroups share a CU.  With one ahead of the other at the issue ports
     // their phases part: while one forms products the other takes exponentials
-    // (64 sequences of 16-node trees 50.7 -> 48.7 us).  Workgroups numbered 256
-    // apart usually meet.
+    // (64 sequences of 16-node trees, heads of 128, 50.7 -> 48.7 us).  Workgroups
+    // numbered 256 apart usually meet.  Ten other loads of four-wave forms, fp32 and
+    // single tokens among them, are within 2% with and without it, but the same
+    // trees with heads of 64: 36.4 us with, 35.2 without.
     if (WAVES == 4 && (blockIdx.x >> 8) & 1) __builtin_amdgcn_s_setprio(2);
     if constexpr (L::kBf16) {
       // (here, where nothing waits for them yet: as they are read, one token takes 9.23 us, not 9.00)
@@ -878,7 +883,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void verify_kernel(AttnVerifyArgs
 // GROUPS groups of D / 4 lanes, four elements a lane, take every GROUPS-th part,
 // kBatch of them read at a time, and meet in LDS.  One pass, bounded by the parts'
 // bytes (from the L2 for the most part) or, for few rows, by its launch and two
-// dependent loads: 3.7 us of the 9.9 us of one token over 1000 keys.
+// dependent loads: 3.8 us of the 9.1 us of one token over 1000 keys.
 template <typename T, int D, int GROUPS>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttnVerifyArgs a, Split split) {
   constexpr int kLanes = D / 4, kSlots = kThreads / kLanes, kBatch = 4;
