@@ -90,3 +90,39 @@ def test_equal_parts_stay_inside(count, hq, hkv, dtype):
     rng = np.random.default_rng(count)
     c = wide(Case(rng.integers(0, 300 if count > 20 else 1500, count), 2, hq, hkv, 64, 64, dtype, seed=count))
     check_verify(c, guarded(c, LONG))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spoilt", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hkv,count,every", [(8, 140, 10), (8, 200, 29), (16, 100, 20), (16, 65, 64), (32, 40, 7)])
+def test_only_long_sequences_are_divided(hkv, count, every, dtype, spoilt):
+    """More sequences than twice the workgroups of a kv head: a few are far longer
+    than a workgroup's even share.  With errors among the divided ones and the whole."""
+    keys, want = (128 if dtype == "bf16" else 64), WORKGROUPS // hkv
+    top = min(40 * want // count - 1, 20) * keys - 3  # shorter than the work that goes in equal parts
+    lens = [top - b % 50 if b % every == every - 1 else b % 30 for b in range(count)]
+    c = Case(lens, 1, hkv, hkv, 64, 16, dtype, seed=count)
+    tiles = [-(-(l + 1) // keys) for l in lens]
+    assert max(tiles) > -(-sum(tiles) // (want // 2)) and count > 2 * want
+    q, k, v, tab = c.dev(c.q), c.dev(c.k), c.dev(c.v), c.dev(c.table)
+    assert B.attn_workspace(q, k, tab, max_len=top).numel() == 4 * want * (66 * hkv + 1) + 8 * count
+    if not spoilt:
+        check_verify(c, guarded(c, top))
+        return
+    status = np.zeros(count, np.int32)
+    parent, table, lens = c.parent.copy(), c.table.copy(), c.lens.copy()
+    for b in list(range(1, count, 5)) + list(range(every - 1, count, 2 * every)):
+        if b % 3 == 0:
+            parent[b, 0], status[b] = 0, B.SLA_ERR_TOPOLOGY
+        elif b % 3 == 1:
+            table[b, int(lens[b]) // 16 // 2], status[b] = -1, B.SLA_ERR_PAGE
+        else:
+            lens[b], status[b] = top + 1, B.SLA_ERR_LENGTH
+    st, out = torch.full((count,), 7, dtype=torch.int32, device="cuda"), torch.full_like(q, float("nan"))
+    B.sla_attn_verify(q, k, v, c.dev(parent), c.dev(table), c.dev(lens), out, max_len=top, status=st,
+                      workspace=B.attn_workspace(q, k, tab, max_len=top))
+    assert st.tolist() == status.tolist()
+    ok = status == 0
+    c.q, c.parent, c.table, c.lens = c.q[ok], c.parent[ok], c.table[ok], c.lens[ok]
+    check_verify(c, out.float().cpu().numpy()[ok])
