@@ -525,6 +525,148 @@ int sla_page_copy(const sla_attn_shape *shape, int32_t layers, void *k_cache, vo
                   const int32_t *src, const int32_t *dst, const int32_t *rows, int32_t copies,
                   int32_t *status, hipStream_t stream);
 
+/* ------------------------------------------------- the prompt pass of a layer
+ *
+ * A prompt, or any run of new tokens that needs no verification, passes a
+ * recurrent layer in four calls: the convolution along each sequence
+ * (sla_conv_prefill), the queries', keys' and gates' final form
+ * (sla_recurrent_inputs), the recurrence over all tokens (sla_prefill), and the
+ * norm and gate of its output (sla_gated_norm).  The second and the fourth work
+ * row by row and serve a draft's nodes as well.
+ *
+ * Packed sequences.  Tokens are rows, one sequence's behind another's:
+ * sequence b has the rows seq_start[b] .. seq_start[b + 1] - 1, seq_start being
+ * device int32 [B + 1].  Sequences may be empty; rows before the first and
+ * behind the last belong to none, and what is written for rows is not written
+ * there.  seq_start must not decrease, begin at 0 or later and end at `tokens`
+ * or earlier; otherwise status[b] is SLA_ERR_LENGTH for every b and nothing but
+ * the status is written.
+ *
+ * States.  A state comes in through one pointer and goes out through another;
+ * both may be the same (in place), else they must not overlap.  No state coming
+ * in (NULL) is a state of zeros.  An empty sequence's state is passed on as it is.
+ *
+ * Strides count elements from row to row; a row's heads are dense, so the
+ * parts of one projection's rows are taken as they are.  What a call writes may
+ * overlap neither another thing it writes nor what it reads, but for a state in
+ * place, else SLA_ERR_ALIAS.  Pointers are 16-byte aligned but for int32 arrays,
+ * gates (alpha, beta, a, b, a_log, dt_bias) and status, strides of q, k, v, x
+ * and z multiples of 16 bytes and of at most 2^22 elements, else
+ * SLA_ERR_UNSUPPORTED.  With no rows (tokens = 0, rows = 0) the pointers to
+ * rows may be NULL.  Results are the same from run to run, and a sequence's do
+ * not depend on the others of its batch. */
+
+typedef struct sla_prefill_shape {
+  int32_t tokens;    /* rows T of q, k, v and out, 0..2^30                     */
+  int32_t batch;     /* sequences B, 1..65535                                  */
+  int32_t heads;     /* H >= 1: heads of v, of the gates and of the state      */
+  int32_t k_heads;   /* heads of q and k, a divisor of H; head h reads the key
+                        head h / (heads / k_heads)                             */
+  int32_t d_k;       /* 64, 128 or 256                                         */
+  int32_t d_v;       /* multiple of 16, 16..1024                               */
+  int32_t qkv_dtype; /* SLA_DTYPE_F32 or SLA_DTYPE_BF16: q, k, v and out       */
+  int32_t family;    /* SLA_FAMILY_GDN, _DELTANET or _DECAY (GLA's gates per
+                        key: SLA_ERR_UNSUPPORTED; sla_verify takes them)       */
+} sla_prefill_shape;
+
+/* sla_prefill -- the recurrence over every sequence's tokens in order:
+ *     S <- the family's step (see SLA_FAMILY_*),   out_t = S q_t.
+ *   state     device fp32 [B][H][d_k][d_v] or NULL (zeros); the layout and
+ *             meaning of sla_verify's.
+ *   q, k      [T][k_heads][d_k]; v [T][H][d_v].
+ *   alpha     device fp32 [T][H], in (0, 1]; not read for DELTANET (may be NULL).
+ *   beta      device fp32 [T][H]; not read for DECAY (may be NULL).
+ *   out       device [T][H][d_v], activation dtype.
+ *   state_out device fp32 [B][H][d_k][d_v].
+ *   workspace device memory of at least sla_prefill_workspace_bytes(shape)
+ *             bytes (may be NULL if that is 0), used until the call's work has
+ *             finished; it needs no initialisation.
+ *   status    device int32 [B] or NULL: 0 or SLA_ERR_LENGTH.
+ * Gates are only multiplied, so any in the range, however small, is valid.
+ * Sums and states are fp32; bf16 activations are read exactly, products with
+ * fp32 values keep 24 bits of those for the state, and 16 for the output, which
+ * is rounded to bf16. */
+int sla_prefill(const sla_prefill_shape *shape, const float *state, const void *q, int64_t q_stride,
+                const void *k, int64_t k_stride, const void *v, int64_t v_stride, const float *alpha,
+                const float *beta, const int32_t *seq_start, void *out, float *state_out, void *workspace,
+                size_t workspace_bytes, int32_t *status, hipStream_t stream);
+
+/* Bytes of sla_prefill's workspace for this shape (0 on a bad shape). */
+size_t sla_prefill_workspace_bytes(const sla_prefill_shape *shape);
+
+typedef struct sla_conv_prefill_shape {
+  int32_t tokens;      /* rows T of x and y, 0..2^30                           */
+  int32_t batch;       /* sequences B, 1..65535                                */
+  int32_t channels;    /* D, a multiple of 8, 8..(1 << 20)                     */
+  int32_t kernel_size; /* K, 1..SLA_CONV_MAX_KERNEL                            */
+  int32_t x_dtype;     /* SLA_DTYPE_F32 or SLA_DTYPE_BF16 (x and y)            */
+  int32_t activation;  /* SLA_ACT_NONE or SLA_ACT_SILU                         */
+} sla_conv_prefill_shape;
+
+/* sla_conv_prefill -- the convolution of sla_conv_verify along every sequence,
+ * behind its conv state, and the state behind its last token.
+ *   conv_state      device fp32 [B][K-1][D], oldest row first, or NULL (zeros).
+ *   x               [T][D] rows x_stride elements apart.
+ *   weight, bias    as in sla_conv_verify: fp32 [D][K], fp32 [D] or NULL.
+ *   y               device [T][D], x's dtype.
+ *   conv_state_out  device fp32 [B][K-1][D] (may be NULL if K = 1).
+ *   status          device int32 [B] or NULL: 0 or SLA_ERR_LENGTH.
+ * The same values, bit for bit, as sla_conv_verify and its commit give. */
+int sla_conv_prefill(const sla_conv_prefill_shape *shape, const float *conv_state, const void *x,
+                     int64_t x_stride, const float *weight, const float *bias, const int32_t *seq_start,
+                     void *y, float *conv_state_out, int32_t *status, hipStream_t stream);
+
+typedef struct sla_inputs_shape {
+  int32_t rows;    /* tokens or nodes N, 0..2^30                               */
+  int32_t heads;   /* heads of the gates, >= 1                                 */
+  int32_t k_heads; /* heads of q and k, >= 1                                   */
+  int32_t repeat;  /* times each head of q and k is written, 1..64             */
+  int32_t d_k;     /* 64, 128 or 256                                           */
+  int32_t dtype;   /* SLA_DTYPE_F32 or SLA_DTYPE_BF16: q, k, a, b and outputs  */
+  float q_scale;   /* finite                                                   */
+  float eps;       /* >= 0                                                     */
+} sla_inputs_shape;
+
+/* sla_recurrent_inputs -- what the recurrence reads, from the projections:
+ *     q_out = q_scale q / sqrt(sum q^2 + eps),  k_out = k / sqrt(sum k^2 + eps)
+ * head by head, each written `repeat` times side by side (q_out, k_out
+ * [N][k_heads repeat][d_k]: a head for every value head, where the reader wants
+ * them so), and the gates
+ *     alpha = exp(-exp(a_log[h]) softplus(a + dt_bias[h])),  beta = sigmoid(b).
+ *   q, k [N][k_heads][d_k]; a, b [N][heads], all with strides of their own.
+ *   a_log, dt_bias  device fp32 [heads] (dt_bias NULL: 0).
+ *   alpha, beta     device fp32 [N][heads].  A layer without one of them passes
+ *     NULL for it and for its input (a and a_log, or b).
+ * Arithmetic is fp32; q_out and k_out are rounded once to the dtype. */
+int sla_recurrent_inputs(const sla_inputs_shape *shape, const void *q, int64_t q_stride, const void *k,
+                         int64_t k_stride, const void *a, int64_t a_stride, const void *b, int64_t b_stride,
+                         const float *a_log, const float *dt_bias, void *q_out, void *k_out, float *alpha,
+                         float *beta, hipStream_t stream);
+
+#define SLA_GATE_NONE 0
+#define SLA_GATE_SILU 1    /* z sigmoid(z) */
+#define SLA_GATE_SIGMOID 2
+
+typedef struct sla_norm_shape {
+  int32_t rows;    /* N, 0..2^30                                               */
+  int32_t heads;   /* >= 1                                                     */
+  int32_t d_v;     /* multiple of 16, 16..1024                                 */
+  int32_t x_dtype; /* SLA_DTYPE_*: x (sla_verify's outputs are fp32)           */
+  int32_t dtype;   /* SLA_DTYPE_*: z and y                                     */
+  int32_t gate;    /* SLA_GATE_*                                               */
+  float eps;       /* >= 0                                                     */
+} sla_norm_shape;
+
+/* sla_gated_norm -- a layer's output, head by head, normalised and gated:
+ *     y = x / sqrt(mean(x^2) + eps) w gate(z)
+ *   x      device [N][heads][d_v]; z [N][heads][d_v], z_stride elements from row
+ *          to row (NULL and not read with SLA_GATE_NONE).
+ *   weight device fp32 [d_v] or NULL (1).
+ *   y      device [N][heads][d_v]; may be x, or z if dense, in the same dtype.
+ * Arithmetic is fp32, rounded once. */
+int sla_gated_norm(const sla_norm_shape *shape, const void *x, const void *z, int64_t z_stride,
+                   const float *weight, void *y, hipStream_t stream);
+
 /* ------------------------------------------------------------ host helpers */
 
 /* Same table as sla_topology for one host-memory parent array, computed

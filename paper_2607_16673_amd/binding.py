@@ -53,6 +53,10 @@ SLA_ACT_SILU = 1
 SLA_CONV_MAX_KERNEL = 4
 SLA_ROPE_HALF = 0
 SLA_ROPE_INTERLEAVED = 1
+SLA_GATE_NONE = 0
+SLA_GATE_SILU = 1
+SLA_GATE_SIGMOID = 2
+GATES = {"none": SLA_GATE_NONE, "silu": SLA_GATE_SILU, "sigmoid": SLA_GATE_SIGMOID}
 ROPE_LAYOUTS = {"half": SLA_ROPE_HALF, "interleaved": SLA_ROPE_INTERLEAVED}
 
 ROUTES = {"auto": SLA_ROUTE_AUTO, "serial": SLA_ROUTE_SERIAL, "parallel": SLA_ROUTE_PARALLEL,
@@ -97,6 +101,29 @@ class SlaAttnTransform(ctypes.Structure):
     _fields_ = [("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float),
                 ("rope", ctypes.c_void_p), ("rope_dim", ctypes.c_int32), ("rope_len", ctypes.c_int32),
                 ("layout", ctypes.c_int32)]
+
+
+class SlaPrefillShape(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("k_heads", ctypes.c_int32), ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32),
+                ("qkv_dtype", ctypes.c_int32), ("family", ctypes.c_int32)]
+
+
+class SlaConvPrefillShape(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("batch", ctypes.c_int32), ("channels", ctypes.c_int32),
+                ("kernel_size", ctypes.c_int32), ("x_dtype", ctypes.c_int32), ("activation", ctypes.c_int32)]
+
+
+class SlaInputsShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("heads", ctypes.c_int32), ("k_heads", ctypes.c_int32),
+                ("repeat", ctypes.c_int32), ("d_k", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("q_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class SlaNormShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("heads", ctypes.c_int32), ("d_v", ctypes.c_int32),
+                ("x_dtype", ctypes.c_int32), ("dtype", ctypes.c_int32), ("gate", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
 
 
 class SlaError(RuntimeError):
@@ -158,6 +185,18 @@ def lib():
         L.sla_attn_commit.restype = ctypes.c_int
         L.sla_page_copy.argtypes = [shape, i32, vp, vp, vp, vp, vp, i32, vp, vp]
         L.sla_page_copy.restype = ctypes.c_int
+        L.sla_prefill.argtypes = [ctypes.POINTER(SlaPrefillShape), vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp,
+                                  size, vp, vp]
+        L.sla_prefill.restype = ctypes.c_int
+        L.sla_prefill_workspace_bytes.argtypes = [ctypes.POINTER(SlaPrefillShape)]
+        L.sla_prefill_workspace_bytes.restype = size
+        L.sla_conv_prefill.argtypes = [ctypes.POINTER(SlaConvPrefillShape), vp, vp, i64, vp, vp, vp, vp, vp, vp, vp]
+        L.sla_conv_prefill.restype = ctypes.c_int
+        L.sla_recurrent_inputs.argtypes = [ctypes.POINTER(SlaInputsShape), vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp,
+                                           vp, vp, vp, vp]
+        L.sla_recurrent_inputs.restype = ctypes.c_int
+        L.sla_gated_norm.argtypes = [ctypes.POINTER(SlaNormShape), vp, vp, i64, vp, vp, vp]
+        L.sla_gated_norm.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -413,6 +452,69 @@ def sla_page_copy(k_cache, v_cache, src, dst, *, rows=None, status=None):
     the cache on the current stream (see sla_page_copy in sla.h)."""
     code = (_nat or native()).page_copy(k_cache, v_cache, src, dst, rows, status)
     _check(code, "sla_page_copy")
+
+
+# --------------------------------------------- the prompt pass of a layer
+def prefill_workspace(q, v, batch: int, *, family: str = "gdn"):
+    """A workspace for sla_prefill calls with these shapes and so many sequences
+    (None if they need none).  One call uses it at a time."""
+    nbytes = (_nat or native()).prefill_workspace_bytes(q, v, batch, FAMILIES[family])
+    return _torch().empty(nbytes, dtype=_torch().uint8, device=q.device) if nbytes else None
+
+
+def sla_prefill(q, k, v, alpha, beta, seq_start, out, state_out, *, state=None, workspace=None, status=None,
+                family: str = "gdn"):
+    """Enqueue the recurrence over packed sequences on the current stream (see
+    sla_prefill in sla.h).
+
+    q, k [T][Hk][dk], v [T][H][dv], each row's heads dense and the rows a constant
+    step apart (parts of one fused projection are taken as they are); alpha, beta
+    [T][H] fp32 (alpha None for "deltanet", beta None for "decay"); seq_start
+    [B + 1] int32; out [T][H][dv]; state_out and state [B][H][dk][dv] fp32, which
+    may be the same tensor (state None: zeros); workspace: from
+    prefill_workspace."""
+    code = (_nat or native()).prefill(q, k, v, alpha, beta, seq_start, out, state_out, state, workspace, status,
+                                      FAMILIES[family])
+    _check(code, "sla_prefill")
+
+
+def sla_conv_prefill(x, weight, seq_start, y, conv_state_out, *, conv_state=None, bias=None, status=None,
+                     activation: bool = True):
+    """Enqueue the short causal convolution along packed sequences on the current
+    stream (see sla_conv_prefill in sla.h).
+
+    x [T][D], its rows a constant step apart; weight [D][K] fp32; seq_start [B + 1]
+    int32; y [T][D]; conv_state_out and conv_state [B][K-1][D] fp32, which may be
+    the same tensor (conv_state None: zeros); bias [D] fp32 or None."""
+    code = (_nat or native()).conv_prefill(x, weight, seq_start, y, conv_state_out, conv_state, bias, status, activation)
+    _check(code, "sla_conv_prefill")
+
+
+def sla_recurrent_inputs(q, k, a, b, a_log, dt_bias, q_out, k_out, alpha, beta, *, q_scale: Optional[float] = None,
+                         eps: float = 1e-6):
+    """Enqueue the recurrence's inputs of N tokens or nodes on the current stream
+    (see sla_recurrent_inputs in sla.h): q_out = q_scale q / |q| and k_out = k / |k|
+    head by head, alpha = exp(-exp(a_log) softplus(a + dt_bias)), beta = sigmoid(b).
+
+    q, k [N][Hk][dk], a, b [N][H], their rows a constant step apart; a_log, dt_bias
+    [H] fp32 (dt_bias may be None); q_out, k_out [N][r Hk][dk], every head r times;
+    alpha, beta [N][H] fp32 (None with its input: not computed).  q_scale defaults
+    to dk^-0.5."""
+    if q_scale is None:
+        q_scale = q.shape[-1] ** -0.5
+    code = (_nat or native()).recurrent_inputs(q, k, a, b, a_log, dt_bias, q_out, k_out, alpha, beta, q_scale, eps)
+    _check(code, "sla_recurrent_inputs")
+
+
+def sla_gated_norm(x, z, weight, y, *, eps: float = 1e-6, gate: str = "silu"):
+    """Enqueue y = x / sqrt(mean(x^2) + eps) weight gate(z), head by head, on the
+    current stream (see sla_gated_norm in sla.h).
+
+    x [N][H][dv] fp32 or bf16; z [N][H][dv], its rows a constant step apart (None
+    with gate "none"); weight [dv] fp32 or None; y [N][H][dv] in z's dtype, which
+    may be x or z."""
+    code = (_nat or native()).gated_norm(x, z, weight, y, eps, GATES[gate])
+    _check(code, "sla_gated_norm")
 
 
 # ------------------------------------------------- draft pruning and packing

@@ -31,7 +31,8 @@ SOURCES = [("verify_tile.hip", "verify_tile_%d_%s_%s" % (dk, form, dt),
            for dk in (128, 256, 64) for form in ("scalar", "gates") for dt in ("bf16", "f32")]
 SOURCES += [(src, os.path.splitext(src)[0], []) for src in
             ("api.cpp", "attn_api.cpp", "attn_append.hip", "attn_cache.hip", "attn_verify.hip", "commit.hip", "conv.hip",
-             "decode.hip", "draft.hip", "verify_serial.hip", "verify_tile_dispatch.cpp")]
+             "conv_prefill.hip", "decode.hip", "draft.hip", "layer_rows.hip", "prefill.hip", "prompt_api.cpp",
+             "verify_serial.hip", "verify_tile_dispatch.cpp")]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-I" + INCLUDE, "-I" + CSRC,
           "-Wall", "-Wno-unused-result",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -14,7 +14,7 @@
 
 namespace {
 
-constexpr int kVersion = 20100;  // 2.1.0: attention over a paged cache
+constexpr int kVersion = 20200;  // 2.2.0: the prompt pass of a recurrent layer
 
 bool dk_ok(int dk) { return dk == 64 || dk == 128 || dk == 256; }
 
@@ -101,7 +101,7 @@ const char *sla_status_string(int status) {
     case SLA_ERR_HIP: return "HIP runtime error";
     case SLA_ERR_SCORE: return "draft log-probability above 0 or NaN";
     case SLA_ERR_PAGE: return "page number outside the pool";
-    case SLA_ERR_LENGTH: return "cache length or row count out of range";
+    case SLA_ERR_LENGTH: return "cache length, sequence start or row count out of range";
     default: return "unknown status";
   }
 }

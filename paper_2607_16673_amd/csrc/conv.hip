@@ -108,13 +108,6 @@ __device__ __forceinline__ void store_f8(float *p, const float (&f)[kCpl]) {
   __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4 *>(p) + 1);
 }
 
-// silu(a) = a / (1 + exp(-a)) with the hardware exp2 and reciprocal (each
-// about 1 ulp): relative error ~1e-6, far below one bf16 rounding and below
-// the fp32 bar.  a -> -inf gives -0 (exp2 overflows to inf, rcp(inf) = 0).
-__device__ __forceinline__ float silu(float a) {
-  return a * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a * -1.4426950408889634f));
-}
-
 // The path of a pending (or standalone) commit, checked against the parent
 // row of the draft it came from; lane t holds step t.  Returns SLA_OK or
 // SLA_ERR_PATH (wave-uniform).  `node` is lane t's node id (clamped).

@@ -1,0 +1,161 @@
+// prefill.hip -- the recurrence over packed sequences, token by token.
+//
+// One workgroup = one (sequence, head) and 64 columns of its state, which stay in
+// registers from the first token to the last: wave w holds the rows w dk / 4 ..,
+// a lane 4 columns of every fourth of them.  With a = S_{t-1} k and b = S_{t-1} q
+// reduced at once, a token needs one exchange between the waves:
+//     u = beta (v - alpha a),  o = alpha b + u (k . q),  S = alpha S + u k^T.
+// Queries, keys and gates of 16 tokens are staged in LDS at a time.  One read and
+// one write of the state bound it for sequences of a token, the chain of
+// exchanges (about a microsecond a token) for longer ones.
+#include "prompt_device.hpp"
+
+namespace sla {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kCols = 64;   // columns of a workgroup
+constexpr int kStage = 16;  // tokens staged at a time
+
+__device__ __forceinline__ void store4(bf16 *p, const float (&x)[4]) {
+  *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+}
+__device__ __forceinline__ void store4(float *p, const float (&x)[4]) {
+  *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+}
+__device__ __forceinline__ void load4(const float *p, float (&x)[4]) { load_f32(p, x); }
+__device__ __forceinline__ void load4(const bf16 *p, float (&x)[4]) {
+  const uint2 w = *reinterpret_cast<const uint2 *>(p);
+  x[0] = __uint_as_float(w.x << 16);
+  x[1] = __uint_as_float(w.x & 0xffff0000u);
+  x[2] = __uint_as_float(w.y << 16);
+  x[3] = __uint_as_float(w.y & 0xffff0000u);
+}
+
+template <typename T, int DK, bool DELTA>
+__global__ __launch_bounds__(kThreads) void serial_kernel(PrefillArgs a, int slabs) {
+  constexpr int kRows = DK / 16;  // of a lane
+  __shared__ float sk[kStage][DK], sq[kStage][DK];
+  __shared__ float salpha[kStage], sbeta[kStage];
+  __shared__ float red[2][4][9][16];  // [parity][wave][a 0-3, b 0-3, k.q][columns of 4]
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int g = lane / 16, cl = lane % 16;
+  const unsigned wg = workgroup();
+  const unsigned unit = wg / (unsigned)slabs;
+  const int slab = (int)(wg % (unsigned)slabs);
+  if (unit >= (unsigned)a.rows.B * (unsigned)a.H) return;
+  const int b = (int)(unit / (unsigned)a.H), h = (int)(unit % (unsigned)a.H);
+  const bool ok = starts_ok(a.rows, lane);
+  if (a.status && h == 0 && slab == 0 && threadIdx.x == 0) a.status[b] = ok ? SLA_OK : SLA_ERR_LENGTH;
+  if (!ok) return;
+  const int start = a.rows.start[b], len = a.rows.start[b + 1] - start;
+  const int col = slab * kCols + cl * 4;
+  const bool live = col < a.dv;
+  const int kh = h / (a.H / a.Hk);
+
+  // lane's row i: wave DK / 4 + 4 i + g
+  float S[kRows][4];
+  const size_t base = ((size_t)unit * DK + wave * (DK / 4) + g) * a.dv + col;
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) S[i][e] = 0.f;
+    if (a.state && live) load4(a.state + base + (size_t)(4 * i) * a.dv, S[i]);
+  }
+  const T *q = static_cast<const T *>(a.q) + (int64_t)start * a.q_stride + (size_t)kh * DK;
+  const T *k = static_cast<const T *>(a.k) + (int64_t)start * a.k_stride + (size_t)kh * DK;
+  const T *v = static_cast<const T *>(a.v) + (int64_t)start * a.v_stride + (size_t)h * a.dv + col;
+  T *out = static_cast<T *>(a.out) + ((size_t)start * a.H + h) * a.dv + col;
+  const size_t gate = (size_t)start * a.H + h;
+
+  for (int t0 = 0; t0 < len; t0 += kStage) {
+    const int n = min(kStage, len - t0);
+    __syncthreads();  // the last stage has been read
+    for (int i = threadIdx.x; i < n * (DK / 8); i += kThreads) {
+      const int t = i / (DK / 8), e = i % (DK / 8) * 8;
+      float x[8];
+      load_f32(k + (int64_t)(t0 + t) * a.k_stride + e, x);
+      store8(&sk[t][e], x);
+      load_f32(q + (int64_t)(t0 + t) * a.q_stride + e, x);
+      store8(&sq[t][e], x);
+    }
+    if (threadIdx.x < n) {
+      salpha[threadIdx.x] = a.alpha ? a.alpha[gate + (size_t)(t0 + threadIdx.x) * a.H] : 1.f;
+      sbeta[threadIdx.x] = DELTA ? a.beta[gate + (size_t)(t0 + threadIdx.x) * a.H] : 1.f;
+    }
+    __syncthreads();
+    for (int t = 0; t < n; ++t) {
+      float x[9] = {};  // S k, S q of 4 columns, k . q
+      float kr[kRows];
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const int r = wave * (DK / 4) + 4 * i + g;
+        kr[i] = sk[t][r];
+        const float qr = sq[t][r];
+        x[8] = __builtin_fmaf(kr[i], qr, x[8]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (DELTA) x[e] = __builtin_fmaf(S[i][e], kr[i], x[e]);
+          x[4 + e] = __builtin_fmaf(S[i][e], qr, x[4 + e]);
+        }
+      }
+#pragma unroll
+      for (int e = DELTA ? 0 : 4; e < 9; ++e) {
+        x[e] += __shfl_xor(x[e], 16);
+        x[e] += __shfl_xor(x[e], 32);
+        if (g == 0) red[t & 1][wave][e][cl] = x[e];
+      }
+      float val[4] = {};
+      if (live) load4(v + (int64_t)(t0 + t) * a.v_stride, val);
+      __syncthreads();
+      float s[9] = {};
+#pragma unroll
+      for (int e = DELTA ? 0 : 4; e < 9; ++e)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) s[e] += red[t & 1][w][e][cl];
+      const float alpha = salpha[t], beta = sbeta[t];
+      float o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float u = DELTA ? beta * (val[e] - alpha * s[e]) : val[e];
+        o[e] = __builtin_fmaf(u, s[8], alpha * s[4 + e]);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) S[i][e] = apply_factor(S[i][e], alpha, kr[i], u);
+      }
+      if (live && threadIdx.x < 16) store4(out + (size_t)(t0 + t) * a.H * a.dv, o);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kRows; ++i)
+    if (live) store4(a.state_out + base + (size_t)(4 * i) * a.dv, S[i]);
+}
+
+template <typename T, int DK>
+hipError_t launch_serial(const PrefillArgs &a, hipStream_t s) {
+  const int slabs = (a.dv + kCols - 1) / kCols;
+  const dim3 grid = grid_of((uint64_t)a.rows.B * a.H * slabs);
+  if (a.family == SLA_FAMILY_DECAY)
+    hipLaunchKernelGGL((serial_kernel<T, DK, false>), grid, dim3(kThreads), 0, s, a, slabs);
+  else
+    hipLaunchKernelGGL((serial_kernel<T, DK, true>), grid, dim3(kThreads), 0, s, a, slabs);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_t(const PrefillArgs &a, hipStream_t s) {
+  switch (a.dk) {
+    case 64: return launch_serial<T, 64>(a, s);
+    case 128: return launch_serial<T, 128>(a, s);
+    default: return launch_serial<T, 256>(a, s);
+  }
+}
+
+}  // namespace
+
+size_t prefill_workspace_bytes(const PrefillArgs &, int) { return 0; }
+
+hipError_t launch_prefill(const PrefillArgs &a, int dtype, hipStream_t s) {
+  return dtype == SLA_DTYPE_BF16 ? launch_t<bf16>(a, s) : launch_t<float>(a, s);
+}
+
+}  // namespace sla

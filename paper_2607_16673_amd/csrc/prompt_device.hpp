@@ -1,0 +1,63 @@
+// prompt_device.hpp -- device-side building blocks of the prompt pass: packed
+// sequences and their division into chunks.
+#pragma once
+
+#include "attn_device.hpp"
+#include "prompt.hpp"
+
+namespace sla {
+
+// Whether the starts are in order and inside the rows (wave-uniform).  Every
+// wave looks at all of them: the loads are independent, 64 sequences at a time.
+__device__ __forceinline__ bool starts_ok(const PackedRows &r, int lane) {
+  bool bad = false;
+  for (int i = lane; i < r.B; i += kWave) {
+    const int a = r.start[i], b = r.start[i + 1];
+    bad = bad || a < 0 || a > b || b > r.tokens;
+  }
+  return !wave_any(bad);
+}
+
+// Chunks of C tokens.  Sequence b's chunk c has the slot start[b] / C + b + c:
+// ceil(len / C) <= end / C - start / C + 1, so no two share one, and no table of
+// chunk counts has to be summed up first.  Some slots stay empty.
+template <int C>
+__host__ __device__ inline int64_t chunk_slots(const PackedRows &r) {
+  return (int64_t)r.tokens / C + r.B;
+}
+
+struct Chunk {
+  int b;      // sequence, -1: none
+  int row;    // first row
+  int rows;   // 1..C, 0: the one chunk of an empty sequence
+  bool first, last;
+};
+
+// The chunk of a slot, of starts that are in order (wave-uniform): b is the
+// last sequence whose first slot is not behind it, counted as in starts_ok.
+// `ok` says whether the starts are in order.
+template <int C>
+__device__ __forceinline__ Chunk find_chunk(const PackedRows &r, int slot, int lane, bool &ok) {
+  bool bad = false;
+  int before = 0;
+  for (int i = lane; i - lane < r.B; i += kWave) {
+    const bool live = i < r.B;
+    const int a = live ? r.start[i] : 0, b = live ? r.start[i + 1] : 0;
+    bad = bad || (live && (a < 0 || a > b || b > r.tokens));
+    before += __popcll(__ballot(live && a / C + i <= slot));
+  }
+  ok = !wave_any(bad);
+  Chunk c = {-1, 0, 0, false, false};
+  if (!ok || before == 0) return c;
+  const int b = before - 1, start = r.start[b], end = r.start[b + 1];
+  const int at = slot - (start / C + b);
+  if (at > 0 && (int64_t)at * C >= end - start) return c;
+  c.b = b;
+  c.row = start + at * C;
+  c.rows = min(C, end - c.row);
+  c.first = at == 0;
+  c.last = c.row + c.rows == end;
+  return c;
+}
+
+}  // namespace sla

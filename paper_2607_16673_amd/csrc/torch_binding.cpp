@@ -13,6 +13,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -501,6 +502,222 @@ PyObject *page_copy(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// The tensors of a prompt-pass call, all on the device of the first.
+class Packed {
+ public:
+  explicit Packed(const at::Tensor &first) : device_(first.device()) {
+    TORCH_CHECK_VALUE(first.is_cuda(), "the tensors must live on the GPU");
+  }
+  c10::Device device() const { return device_; }
+  template <typename P = void>
+  P *dense(PyObject *o, at::ScalarType dtype, Dims shape, const char *name) const {
+    void *const p = pointer(o, dtype, shape, name);
+    same(THPVariable_Unpack(o), name);
+    return static_cast<P *>(p);
+  }
+  template <typename P = void>
+  P *optional(PyObject *o, at::ScalarType dtype, Dims shape, const char *name) const {
+    return o == Py_None ? nullptr : dense<P>(o, dtype, shape, name);
+  }
+  // [rows][..] whose rows are dense and a constant step apart (parts of a wider row)
+  const void *rows(PyObject *o, at::ScalarType dtype, Dims shape, const char *name, int64_t &step) const {
+    const at::Tensor &t = tensor(o, name);
+    same(t, name);
+    TORCH_CHECK_TYPE(t.scalar_type() == dtype, name, " must be ", dtype, ", got ", t.scalar_type());
+    const at::IntArrayRef want(shape.begin(), shape.size());
+    TORCH_CHECK_VALUE(t.sizes() == want, name, " has shape ", t.sizes(), ", expected ", want);
+    int64_t width = 1;
+    bool dense = true;
+    for (int64_t d = t.dim() - 1; d > 0; --d) {
+      dense = dense && (t.size(d) == 1 || t.stride(d) == width);
+      width *= t.size(d);
+    }
+    step = t.size(0) > 1 ? t.stride(0) : width;
+    TORCH_CHECK_VALUE(t.numel() == 0 || (dense && step >= width), name,
+                      " must hold each row contiguously, its rows a constant step apart; strides are ", t.strides());
+    if (t.numel() == 0) step = width;
+    return t.data_ptr();
+  }
+
+ private:
+  void same(const at::Tensor &t, const char *name) const {
+    TORCH_CHECK_VALUE(t.device() == device_, name, " must live on ", device_, ", not ", t.device());
+  }
+  c10::Device device_;
+};
+
+int32_t size32(int64_t n, const char *name) {
+  TORCH_CHECK_VALUE(n <= INT32_MAX, name, " is too large: ", n);
+  return (int32_t)n;
+}
+
+float real(PyObject *o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw python_error();
+  return (float)v;
+}
+
+sla_prefill_shape prefill_shape(const at::Tensor &q, const at::Tensor &v, int64_t batch, int32_t family) {
+  sla_prefill_shape s;
+  s.tokens = size32(q.size(0), "tokens");
+  s.batch = size32(batch, "batch");
+  s.heads = size32(v.size(1), "heads");
+  s.k_heads = size32(q.size(1), "k_heads");
+  s.d_k = size32(q.size(2), "d_k");
+  s.d_v = size32(v.size(2), "d_v");
+  s.qkv_dtype = activation_code(q);
+  s.family = family;
+  return s;
+}
+
+// prefill(q, k, v, alpha | None, beta | None, seq_start, out, state_out, state | None, workspace | None, status | None,
+//         family)
+PyObject *prefill(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  count_args(nargs, 12);
+  const at::Tensor &q = sized(o[0], 3, "q"), &v = sized(o[2], 3, "v"), &starts = sized(o[5], 1, "seq_start");
+  TORCH_CHECK_VALUE(starts.size(0) > 1, "seq_start has shape ", starts.sizes(), ", expected [sequences + 1]");
+  const int64_t T = q.size(0), kh = q.size(1), dk = q.size(2), H = v.size(1), dv = v.size(2), B = starts.size(0) - 1;
+  const at::ScalarType act = q.scalar_type();
+  const sla_prefill_shape shape = prefill_shape(q, v, B, number32(o[11], "family"));
+  const Packed r(q);
+  int64_t qs, ks, vs;
+  const void *qp = r.rows(o[0], act, {T, kh, dk}, "q", qs);
+  const void *kp = r.rows(o[1], act, {T, kh, dk}, "k", ks);
+  const void *vp = r.rows(o[2], act, {T, H, dv}, "v", vs);
+  const float *alpha = r.optional<float>(o[3], at::kFloat, {T, H}, "alpha");
+  const float *beta = r.optional<float>(o[4], at::kFloat, {T, H}, "beta");
+  const int32_t *start = r.dense<int32_t>(o[5], at::kInt, {B + 1}, "seq_start");
+  void *out = r.dense(o[6], act, {T, H, dv}, "out");
+  float *state_out = r.dense<float>(o[7], at::kFloat, {B, H, dk, dv}, "state_out");
+  const float *state = r.optional<float>(o[8], at::kFloat, {B, H, dk, dv}, "state");
+  void *ws = nullptr;
+  size_t bytes = 0;
+  if (o[9] != Py_None) {
+    bytes = (size_t)sized(o[9], 1, "workspace").size(0);
+    ws = r.dense(o[9], at::kByte, {(int64_t)bytes}, "workspace");
+  }
+  int32_t *status = r.optional<int32_t>(o[10], at::kInt, {B}, "status");
+  const c10::DeviceGuard guard(r.device());
+  const hipStream_t stream = stream_of(q);
+  return PyLong_FromLong(unlocked([&] {
+    return sla_prefill(&shape, state, qp, qs, kp, ks, vp, vs, alpha, beta, start, out, state_out, ws, bytes, status,
+        stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+// prefill_workspace_bytes(q, v, batch, family)
+PyObject *prefill_workspace_bytes(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  count_args(nargs, 4);
+  const at::Tensor &q = sized(o[0], 3, "q"), &v = sized(o[1], 3, "v");
+  const sla_prefill_shape shape = prefill_shape(q, v, number(o[2]), number32(o[3], "family"));
+  const c10::DeviceGuard guard(Packed(q).device());
+  return PyLong_FromSize_t(sla_prefill_workspace_bytes(&shape));
+  END_HANDLE_TH_ERRORS
+}
+
+// conv_prefill(x, weight, seq_start, y, conv_state_out | None, conv_state | None, bias | None, status | None, activation)
+PyObject *conv_prefill(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  count_args(nargs, 9);
+  const at::Tensor &x = sized(o[0], 2, "x"), &w = sized(o[1], 2, "weight"), &starts = sized(o[2], 1, "seq_start");
+  TORCH_CHECK_VALUE(starts.size(0) > 1, "seq_start has shape ", starts.sizes(), ", expected [sequences + 1]");
+  const int64_t T = x.size(0), D = x.size(1), K = w.size(1), B = starts.size(0) - 1;
+  const at::ScalarType act = x.scalar_type();
+  sla_conv_prefill_shape shape;
+  shape.tokens = size32(T, "tokens");
+  shape.batch = size32(B, "batch");
+  shape.channels = size32(D, "channels");
+  shape.kernel_size = size32(K, "kernel_size");
+  shape.x_dtype = activation_code(x);
+  shape.activation = truth(o[8]) ? SLA_ACT_SILU : SLA_ACT_NONE;
+  const Packed r(x);
+  int64_t xs;
+  const void *xp = r.rows(o[0], act, {T, D}, "x", xs);
+  const float *wp = r.dense<float>(o[1], at::kFloat, {D, K}, "weight");
+  const int32_t *start = r.dense<int32_t>(o[2], at::kInt, {B + 1}, "seq_start");
+  void *y = r.dense(o[3], act, {T, D}, "y");
+  float *state_out = r.optional<float>(o[4], at::kFloat, {B, K - 1, D}, "conv_state_out");
+  const float *state = r.optional<float>(o[5], at::kFloat, {B, K - 1, D}, "conv_state");
+  const float *bias = r.optional<float>(o[6], at::kFloat, {D}, "bias");
+  int32_t *status = r.optional<int32_t>(o[7], at::kInt, {B}, "status");
+  const c10::DeviceGuard guard(r.device());
+  const hipStream_t stream = stream_of(x);
+  return PyLong_FromLong(unlocked([&] {
+    return sla_conv_prefill(&shape, state, xp, xs, wp, bias, start, y, state_out, status, stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+// recurrent_inputs(q, k, a | None, b | None, a_log | None, dt_bias | None, q_out, k_out, alpha | None, beta | None, q_scale,
+//                  eps)
+PyObject *recurrent_inputs(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  count_args(nargs, 12);
+  const at::Tensor &q = sized(o[0], 3, "q"), &qo = sized(o[6], 3, "q_out");
+  const int64_t N = q.size(0), kh = q.size(1), dk = q.size(2), oh = qo.size(1);
+  TORCH_CHECK_VALUE(kh > 0 && oh % kh == 0, "q_out has ", oh, " heads, expected a multiple of q's ", kh);
+  PyObject *const gate = o[8] != Py_None ? o[8] : o[9];
+  const int64_t H = gate != Py_None ? sized(gate, 2, "alpha or beta").size(1) : 1;
+  const at::ScalarType act = q.scalar_type();
+  sla_inputs_shape shape;
+  shape.rows = size32(N, "rows");
+  shape.heads = size32(H, "heads");
+  shape.k_heads = size32(kh, "k_heads");
+  shape.repeat = size32(oh / kh, "repeat");
+  shape.d_k = size32(dk, "d_k");
+  shape.dtype = activation_code(q);
+  shape.q_scale = real(o[10]);
+  shape.eps = real(o[11]);
+  const Packed r(q);
+  int64_t qs, ks, as = H, bs = H;
+  const void *qp = r.rows(o[0], act, {N, kh, dk}, "q", qs);
+  const void *kp = r.rows(o[1], act, {N, kh, dk}, "k", ks);
+  const void *ap = o[2] == Py_None ? nullptr : r.rows(o[2], act, {N, H}, "a", as);
+  const void *bp = o[3] == Py_None ? nullptr : r.rows(o[3], act, {N, H}, "b", bs);
+  const float *a_log = r.optional<float>(o[4], at::kFloat, {H}, "a_log");
+  const float *dt_bias = r.optional<float>(o[5], at::kFloat, {H}, "dt_bias");
+  void *q_out = r.dense(o[6], act, {N, oh, dk}, "q_out");
+  void *k_out = r.dense(o[7], act, {N, oh, dk}, "k_out");
+  float *alpha = r.optional<float>(o[8], at::kFloat, {N, H}, "alpha");
+  float *beta = r.optional<float>(o[9], at::kFloat, {N, H}, "beta");
+  const c10::DeviceGuard guard(r.device());
+  const hipStream_t stream = stream_of(q);
+  return PyLong_FromLong(unlocked([&] {
+    return sla_recurrent_inputs(&shape, qp, qs, kp, ks, ap, as, bp, bs, a_log, dt_bias, q_out, k_out, alpha, beta, stream);
+  }));
+  END_HANDLE_TH_ERRORS
+}
+
+// gated_norm(x, z | None, weight | None, y, eps, gate)
+PyObject *gated_norm(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  count_args(nargs, 6);
+  const at::Tensor &x = sized(o[0], 3, "x"), &y = sized(o[3], 3, "y");
+  const int64_t N = x.size(0), H = x.size(1), dv = x.size(2);
+  const at::ScalarType act = y.scalar_type();
+  sla_norm_shape shape;
+  shape.rows = size32(N, "rows");
+  shape.heads = size32(H, "heads");
+  shape.d_v = size32(dv, "d_v");
+  shape.x_dtype = activation_code(x);
+  shape.dtype = activation_code(y);
+  shape.eps = real(o[4]);
+  shape.gate = number32(o[5], "gate");
+  const Packed r(x);
+  int64_t zs = H * dv;
+  const void *xp = r.dense(o[0], x.scalar_type(), {N, H, dv}, "x");
+  const void *zp = o[1] == Py_None ? nullptr : r.rows(o[1], act, {N, H, dv}, "z", zs);
+  const float *w = r.optional<float>(o[2], at::kFloat, {dv}, "weight");
+  void *yp = r.dense(o[3], act, {N, H, dv}, "y");
+  const c10::DeviceGuard guard(r.device());
+  const hipStream_t stream = stream_of(x);
+  return PyLong_FromLong(unlocked([&] { return sla_gated_norm(&shape, xp, zp, zs, w, yp, stream); }));
+  END_HANDLE_TH_ERRORS
+}
+
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)>
 constexpr PyMethodDef method(const char *name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
@@ -516,6 +733,11 @@ PyMethodDef methods[] = {method<verify>("verify"),
                          method<attn_workspace_bytes>("attn_workspace_bytes"),
                          method<attn_commit>("attn_commit"),
                          method<page_copy>("page_copy"),
+                         method<prefill>("prefill"),
+                         method<prefill_workspace_bytes>("prefill_workspace_bytes"),
+                         method<conv_prefill>("conv_prefill"),
+                         method<recurrent_inputs>("recurrent_inputs"),
+                         method<gated_norm>("gated_norm"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of libsla's device calls.", -1, methods};
