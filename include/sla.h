@@ -585,7 +585,8 @@ typedef struct sla_prefill_shape {
  * Gates are only multiplied, so any in the range, however small, is valid.
  * Sums and states are fp32; bf16 activations are read exactly, products with
  * fp32 values keep 24 bits of those for the state, and 16 for the output, which
- * is rounded to bf16. */
+ * is rounded to bf16.  A NaN or an infinity in a sequence's rows spoils all its
+ * outputs from the first one of its chunk of 64 tokens on, and its state. */
 int sla_prefill(const sla_prefill_shape *shape, const float *state, const void *q, int64_t q_stride,
                 const void *k, int64_t k_stride, const void *v, int64_t v_stride, const float *alpha,
                 const float *beta, const int32_t *seq_start, void *out, float *state_out, void *workspace,

@@ -29,6 +29,8 @@ ARCH = "gfx950"
 SOURCES = [("verify_tile.hip", "verify_tile_%d_%s_%s" % (dk, form, dt),
             ["-DSLA_TILE_DK=%d" % dk, "-DSLA_TILE_GATES=%d" % (form == "gates"), "-DSLA_TILE_F32=%d" % (dt == "f32")])
            for dk in (128, 256, 64) for form in ("scalar", "gates") for dt in ("bf16", "f32")]
+SOURCES += [("prefill_chunk.hip", "prefill_chunk_%d_%s" % (dk, dt),
+             ["-DSLA_CHUNK_DK=%d" % dk, "-DSLA_CHUNK_F32=%d" % (dt == "f32")]) for dk in (256, 128, 64) for dt in ("f32", "bf16")]
 SOURCES += [(src, os.path.splitext(src)[0], []) for src in
             ("api.cpp", "attn_api.cpp", "attn_append.hip", "attn_cache.hip", "attn_verify.hip", "commit.hip", "conv.hip",
              "conv_prefill.hip", "decode.hip", "draft.hip", "layer_rows.hip", "prefill.hip", "prompt_api.cpp",

@@ -8,7 +8,9 @@
 // Queries, keys and gates of 16 tokens are staged in LDS at a time.  One read and
 // one write of the state bound it for sequences of a token, the chain of
 // exchanges (about a microsecond a token) for longer ones.
-#include "prompt_device.hpp"
+#include <type_traits>
+
+#include "prefill_chunk.hpp"
 
 namespace sla {
 namespace {
@@ -141,21 +143,43 @@ hipError_t launch_serial(const PrefillArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T>
+// Sequences of about a token take the serial kernel: it streams the states once,
+// in one launch, where the chunked ones need a chunk's matrices first.
+bool serial(const PrefillArgs &a) { return a.rows.tokens <= 4 * (int64_t)a.rows.B; }
+
+template <bool F32, int DK>
+hipError_t launch_dk(const PrefillArgs &a, hipStream_t s) {
+  using T = typename std::conditional<F32, float, bf16>::type;
+  return serial(a) ? launch_serial<T, DK>(a, s) : launch_chunks<F32, DK>(a, s);
+}
+
+template <bool F32>
 hipError_t launch_t(const PrefillArgs &a, hipStream_t s) {
   switch (a.dk) {
-    case 64: return launch_serial<T, 64>(a, s);
-    case 128: return launch_serial<T, 128>(a, s);
-    default: return launch_serial<T, 256>(a, s);
+    case 64: return launch_dk<F32, 64>(a, s);
+    case 128: return launch_dk<F32, 128>(a, s);
+    default: return launch_dk<F32, 256>(a, s);
+  }
+}
+
+template <bool F32>
+size_t bytes_t(const PrefillArgs &a) {
+  switch (a.dk) {
+    case 64: return chunk_space<F32, 64>(a).bytes();
+    case 128: return chunk_space<F32, 128>(a).bytes();
+    default: return chunk_space<F32, 256>(a).bytes();
   }
 }
 
 }  // namespace
 
-size_t prefill_workspace_bytes(const PrefillArgs &, int) { return 0; }
+size_t prefill_workspace_bytes(const PrefillArgs &a, int dtype) {
+  if (serial(a)) return 0;
+  return dtype == SLA_DTYPE_BF16 ? bytes_t<false>(a) : bytes_t<true>(a);
+}
 
 hipError_t launch_prefill(const PrefillArgs &a, int dtype, hipStream_t s) {
-  return dtype == SLA_DTYPE_BF16 ? launch_t<bf16>(a, s) : launch_t<float>(a, s);
+  return dtype == SLA_DTYPE_BF16 ? launch_t<false>(a, s) : launch_t<true>(a, s);
 }
 
 }  // namespace sla

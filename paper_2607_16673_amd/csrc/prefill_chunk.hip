@@ -1,0 +1,587 @@
+// prefill_chunk.hip -- the recurrence over packed sequences in chunks of 64
+// tokens on the matrix cores (specialised by SLA_CHUNK_DK and SLA_CHUNK_F32).
+//
+// With D_ij the product of the gates j + 1 .. i and G_i of those up to i (from
+// the chunk's start), H the state in front of it, Q, K, V its rows:
+//     X = (I + L)^-1,  L_ij = beta_i D_ij k_i . k_j  (j < i)
+//     R = V - G o (K H)
+//     out = G o (Q H) + [(D o Q K^T, lower) X beta] R
+//     H' = G_63 H + K^T [D_63 o X beta] R
+// The matrices in brackets do not depend on the state.  A first kernel makes them
+// for all chunks at once; a second walks each sequence's chunks in order.  Gates
+// are only multiplied: no logarithm, no quotient, so tiny ones do no harm.
+//
+// A sequence's NaN or infinity reaches all outputs of its chunk of 64 tokens, those
+// of earlier tokens in it included, and no other sequence.
+#include <type_traits>
+
+#include "prefill_chunk.hpp"
+
+namespace sla {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPitch = 68;  // of a 64 x 64 fp32 matrix in LDS
+
+// workgroup barrier for LDS: loads from memory stay in flight across it
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// ------------------------------------------------------------ first kernel
+// One workgroup = one chunk and one head.  Wave w owns the matrices' rows 16 w ..
+// Rows past the sequence's end count as zero keys with gate 1 and strength 0.
+template <bool F32, int DK>
+struct MatricesLds {
+  using T = typename std::conditional<F32, float, bf16>::type;
+  static constexpr int kKeyPitch = DK + 16 / (int)sizeof(T);
+  T k[kChunk * kKeyPitch];
+  float x[kChunk * kPitch];  // L, then X
+  float p[kChunk * kPitch];  // D o Q K^T, then times X beta
+  float d[4][16][16];        // D inside the diagonal blocks
+  float upto[kChunk];        // product of a block's gates up to i
+  float behind[kChunk];      // product of a block's gates behind j
+  float total[4];            // of a block's gates
+  float decay[kChunk];       // G
+  float rest[kChunk];        // D_63
+  float beta[kChunk];
+};
+
+// row r's 4 inner indices 4 g + e of a 16 x 16 block
+__device__ __forceinline__ f32x4 block_a(const float *m, int bi, int bj, int g, int r) {
+  return *reinterpret_cast<const f32x4 *>(m + (16 * bi + r) * kPitch + 16 * bj + 4 * g);
+}
+__device__ __forceinline__ f32x4 block_b(const float *m, int bi, int bj, int g, int r) {
+  f32x4 x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = m[(16 * bi + 4 * g + e) * kPitch + 16 * bj + r];
+  return x;
+}
+__device__ __forceinline__ void block_store(float *m, int bi, int bj, int g, int r, f32x4 x) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m[(16 * bi + 4 * g + e) * kPitch + 16 * bj + r] = x[e];
+}
+// c + a b of 16 x 16 blocks, inner index 4 g + e
+__device__ __forceinline__ f32x4 block_mma(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+
+// 8 neighbouring values as an operand of N planes, 16 bytes a lane and piece
+template <bool F32, int N>
+__device__ __forceinline__ void store_frag(unsigned char *at, int lane, const float (&x)[8]) {
+  if constexpr (F32) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      *reinterpret_cast<f32x4 *>(at + (i * kWave + lane) * 16) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+  } else {
+    const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
+    uint2 a[N], b[N];
+    split4(lo, a);
+    split4(hi, b);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      *reinterpret_cast<uint4 *>(at + (n * kWave + lane) * 16) = make_uint4(a[n].x, a[n].y, b[n].x, b[n].y);
+  }
+}
+
+template <bool F32, int DK, bool DELTA>
+__global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
+  using L = MatricesLds<F32, DK>;
+  using T = typename L::T;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  L &s = *reinterpret_cast<L *>(lds);
+  const ChunkSpace<F32, DK> space = chunk_space<F32, DK>(a);
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int g = lane / 16, r = lane % 16;
+  const unsigned wg = workgroup();
+  const unsigned slot = wg / (unsigned)a.H;
+  const int h = (int)(wg % (unsigned)a.H), group = a.H / a.Hk, kh = h / group;
+  if (slot >= space.slots) return;
+  bool ok;
+  const Chunk c = find_chunk<kChunk>(a.rows, (int)slot, lane, ok);
+  if (c.b < 0 || c.rows == 0) return;
+
+  // keys to LDS, queries to registers, gates
+  constexpr int kLanes = DK / 8;
+  const T *k = static_cast<const T *>(a.k) + (int64_t)c.row * a.k_stride + (size_t)kh * DK;
+  for (int i = threadIdx.x; i < kChunk * kLanes; i += kThreads) {
+    const int t = i / kLanes, e = i % kLanes * 8;
+    u32x4 *to = reinterpret_cast<u32x4 *>(s.k + t * L::kKeyPitch + e);
+    const u32x4 *from = reinterpret_cast<const u32x4 *>(k + (int64_t)t * a.k_stride + e);
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) to[j] = t < c.rows ? from[j] : u32x4{0, 0, 0, 0};
+  }
+  Frag<F32, 1> q[DK / 32];
+  {
+    const int t = 16 * wave + r;
+    const T *row = static_cast<const T *>(a.q) + (int64_t)(c.row + min(t, c.rows - 1)) * a.q_stride + (size_t)kh * DK + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < DK / 32; ++ks)
+#pragma unroll
+      for (int j = 0; j < kPiecesOf<F32, 1>; ++j) {
+        u32x4 x = reinterpret_cast<const u32x4 *>(row + 32 * ks)[j];
+        if (t >= c.rows) x = u32x4{0, 0, 0, 0};
+        reinterpret_cast<u32x4 *>(&q[ks])[j] = x;
+      }
+  }
+  const size_t gate = (size_t)c.row * a.H + h;
+  if (wave == 1) s.beta[lane] = lane < c.rows ? (DELTA ? a.beta[gate + (size_t)lane * a.H] : 1.f) : 0.f;
+  if (wave == 0) {
+    // lane 16 b + j: column j of D's diagonal block b, and the products along the block
+    const float al = a.alpha && lane < c.rows ? a.alpha[gate + (size_t)lane * a.H] : 1.f;
+    float col = 0.f, run = 1.f, upto = 1.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float ai = __shfl(al, (lane & 48) + i);
+      col = i == r ? 1.f : col * ai;
+      run *= ai;
+      if (i == r) upto = run;
+      s.d[g][i][r] = i >= r ? col : 0.f;
+    }
+    const float t0 = __shfl(upto, 15), t1 = __shfl(upto, 31), t2 = __shfl(upto, 47), t3 = __shfl(upto, 63);
+    const float front = g == 0 ? 1.f : g == 1 ? t0 : g == 2 ? t0 * t1 : t0 * t1 * t2;
+    const float back = g == 3 ? 1.f : g == 2 ? t3 : g == 1 ? t2 * t3 : t1 * t2 * t3;
+    s.upto[lane] = upto;
+    s.behind[lane] = col;
+    if (r == 15) s.total[g] = upto;
+    s.decay[lane] = front * upto;
+    s.rest[lane] = col * back;
+  }
+  lds_barrier();
+
+  // K K^T and Q K^T, decayed: row tile `wave`, column tiles up to it
+  {
+    Frag<F32, 1> kr[DK / 32];
+#pragma unroll
+    for (int ks = 0; ks < DK / 32; ++ks)
+#pragma unroll
+      for (int j = 0; j < kPiecesOf<F32, 1>; ++j)
+        reinterpret_cast<u32x4 *>(&kr[ks])[j] =
+            reinterpret_cast<const u32x4 *>(s.k + (16 * wave + r) * L::kKeyPitch + 32 * ks + 8 * g)[j];
+    float mid = 1.f;  // product of the blocks between the columns' and the rows'
+    for (int t = wave; t >= 0; --t) {
+      f32x4 kk = {0.f, 0.f, 0.f, 0.f}, qk = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < DK / 32; ++ks) {
+        Frag<F32, 1> col;
+#pragma unroll
+        for (int j = 0; j < kPiecesOf<F32, 1>; ++j)
+          reinterpret_cast<u32x4 *>(&col)[j] =
+              reinterpret_cast<const u32x4 *>(s.k + (16 * t + r) * L::kKeyPitch + 32 * ks + 8 * g)[j];
+        if (DELTA) kk = mma<1, 1>(kr[ks], col, kk);
+        qk = mma<1, 1>(q[ks], col, qk);
+      }
+      const float behind = s.behind[16 * t + r] * mid;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = 16 * wave + 4 * g + i;
+        const float d = t == wave ? s.d[wave][4 * g + i][r] : s.upto[row] * behind;
+        if (DELTA) s.x[row * kPitch + 16 * t + r] = t == wave && 4 * g + i <= r ? 0.f : s.beta[row] * d * kk[i];
+        s.p[row * kPitch + 16 * t + r] = t == wave && 4 * g + i < r ? 0.f : d * qk[i];
+      }
+      if (t < wave) mid *= s.total[t];
+    }
+    if (wave % 2 == 0) {  // right of the diagonal: the operands reach there
+      block_store(s.x, wave, wave + 1, g, r, f32x4{0.f, 0.f, 0.f, 0.f});
+      block_store(s.p, wave, wave + 1, g, r, f32x4{0.f, 0.f, 0.f, 0.f});
+    }
+  }
+
+  if constexpr (DELTA) {
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    lds_barrier();
+    {  // diagonal blocks: column r by forward substitution, in every 16 lanes alike
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[i] = i == r ? 1.f : 0.f;
+#pragma unroll
+        for (int j4 = 0; j4 < (i + 3) / 4; ++j4) {
+          const f32x4 l = *reinterpret_cast<const f32x4 *>(s.x + (16 * wave + i) * kPitch + 16 * wave + 4 * j4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (4 * j4 + j < i) x[i] = __builtin_fmaf(-l[j], x[4 * j4 + j], x[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (i / 4 == g) s.x[(16 * wave + i) * kPitch + 16 * wave + r] = x[i];
+    }
+    lds_barrier();
+    if (wave < 2) {  // X10 = -X11 L10 X00, X32 likewise
+      const int b = 2 * wave;
+      const f32x4 y = block_mma(block_a(s.x, b + 1, b, g, r), block_b(s.x, b, b, g, r), zero);
+      block_store(s.x, b + 1, b, g, r, -block_mma(block_a(s.x, b + 1, b + 1, g, r), y, zero));
+    }
+    lds_barrier();
+    f32x4 y2 = zero, y3 = zero;  // rows 2, 3 of L X, column `wave`
+    if (wave < 2) {
+      for (int m = wave; m < 2; ++m) {
+        const f32x4 x = block_b(s.x, m, wave, g, r);
+        y2 = block_mma(block_a(s.x, 2, m, g, r), x, y2);
+        y3 = block_mma(block_a(s.x, 3, m, g, r), x, y3);
+      }
+    }
+    lds_barrier();
+    if (wave < 2) {
+      block_store(s.x, 2, wave, g, r, -block_mma(block_a(s.x, 2, 2, g, r), y2, zero));
+      block_store(s.x, 3, wave, g, r,
+                  -block_mma(block_a(s.x, 3, 3, g, r), y3, block_mma(block_a(s.x, 3, 2, g, r), y2, zero)));
+    }
+    lds_barrier();
+    f32x4 px[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      px[t] = zero;
+      if (t > wave) continue;
+      for (int m = t; m <= wave; ++m) px[t] = block_mma(block_a(s.p, wave, m, g, r), block_b(s.x, m, t, g, r), px[t]);
+      px[t] *= s.beta[16 * t + r];
+    }
+    // a row tile's blocks have one reader and writer, its wave
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (t <= wave) block_store(s.p, wave, t, g, r, px[t]);
+  }
+  lds_barrier();
+
+  // out: row tile `wave` as the second kernel's operands
+  unsigned char *head = space.head(slot, h);
+  const int row = tile_row(wave, r);
+  const float rest = s.rest[row];
+  for (int ks = 0; ks <= wave / 2; ++ks) {
+    const int f = first_frag(wave) + ks, at = 32 * ks + 8 * g;
+    float x[8], p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = DELTA ? s.x[row * kPitch + at + e] * s.beta[at + e] * rest : at + e == row ? rest : 0.f;
+      p[e] = s.p[row * kPitch + at + e];
+    }
+    store_frag<F32, kStatePlanes>(head + (size_t)f * kPiecesOf<F32, kStatePlanes> * space.kPiece, lane, x);
+    store_frag<F32, kOutPlanes>(head + space.kToState + (size_t)f * kPiecesOf<F32, kOutPlanes> * space.kPiece, lane, p);
+  }
+  if (threadIdx.x < kChunk)
+    reinterpret_cast<float *>(head + space.kToState + space.kToOut)[threadIdx.x] = s.decay[threadIdx.x];
+  if (h % group == 0) {
+    unsigned char *keys = space.keys(slot, kh);
+    for (int f = wave; f < DK / 16 * 2; f += kThreads / kWave) {
+      const T *from = s.k + (32 * (f % 2) + 8 * g) * L::kKeyPitch + tile_row(f / 2, r);
+      unsigned char *to = keys + (size_t)f * kPiecesOf<F32, 1> * space.kPiece;
+      if constexpr (F32) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = from[e * L::kKeyPitch];
+        store_frag<true, 1>(to, lane, x);
+      } else {
+        uint32_t x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = from[e * L::kKeyPitch].bits;
+        *reinterpret_cast<uint4 *>(to + lane * 16) =
+            make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
+      }
+    }
+  }
+}
+
+// ----------------------------------------------------------- second kernel
+// One workgroup = one (sequence, head) and 16 NT columns of its state, which stay
+// in the accumulators of its four waves from the first chunk to the last: wave w
+// has the row tiles w, w + 4, .. of d_k.  Of a chunk it has the token tile w.  The
+// state, R and the corrected values pass through LDS as operands, three barriers
+// a chunk; what comes from memory is asked for as soon as the chunk before has
+// used its registers.
+//
+// Columns: lane r of column tile n has the column 32 (n / 2) + 8 (r / 4) + 4 (n % 2)
+// + r % 4 of the slab, so that an output tile, made transposed, gives each lane 8
+// neighbouring columns of a token.
+template <bool F32, int DK, int NT>
+struct StateLds {
+  static constexpr int kPieces = kPiecesOf<F32, kStatePlanes>;
+  static constexpr size_t kFrag = (size_t)kPieces * kWave * 16;
+  static constexpr int kStateFrags = DK / 32 * NT, kRowFrags = 2 * NT;
+  static constexpr size_t kBytes = (kStateFrags + 2 * kRowFrags) * kFrag;
+};
+
+// half `half` (4 of 8 values) of a lane's operand
+template <bool F32>
+__device__ __forceinline__ void put_half(unsigned char *frag, int half, int lane, f32x4 x) {
+  if constexpr (F32) {
+    *reinterpret_cast<f32x4 *>(frag + (half * kWave + lane) * 16) = x;
+  } else {
+    const float v[4] = {x[0], x[1], x[2], x[3]};
+    uint2 p[kStatePlanes];
+    split4(v, p);
+#pragma unroll
+    for (int n = 0; n < kStatePlanes; ++n) *reinterpret_cast<uint2 *>(frag + (n * kWave + lane) * 16 + 8 * half) = p[n];
+  }
+}
+
+template <bool F32, int N>
+__device__ __forceinline__ Frag<F32, N> get_frag(const unsigned char *frag, int lane) {
+  Frag<F32, N> f;
+#pragma unroll
+  for (int n = 0; n < kPiecesOf<F32, N>; ++n)
+    reinterpret_cast<u32x4 *>(&f)[n] = *reinterpret_cast<const u32x4 *>(frag + (n * kWave + lane) * 16);
+  return f;
+}
+
+__device__ __forceinline__ u32x4 buf_load16(rsrc_t r, uint32_t voff, uint32_t soff) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, kPolicyDefault));
+}
+
+constexpr uint32_t kNowhere = 0x7fffffffu;  // an offset past any chunk's rows: reads give 0, writes are dropped
+
+template <bool F32, int DK, int NT, bool DELTA>
+__global__ __launch_bounds__(kThreads) void state_kernel(PrefillArgs a, int slabs) {
+  using T = typename std::conditional<F32, float, bf16>::type;
+  using L = StateLds<F32, DK, NT>;
+  constexpr int kKs = DK / 32, kTiles = DK / 64, w = sizeof(T);
+  constexpr int kKeyPieces = kPiecesOf<F32, 1>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  unsigned char *const lds_h = lds, *const lds_r = lds + L::kStateFrags * L::kFrag, *const lds_u = lds_r + L::kRowFrags * L::kFrag;
+  const ChunkSpace<F32, DK> space = chunk_space<F32, DK>(a);
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int g = lane / 16, r = lane % 16;
+  const int half = wave % 2;  // of the token tile `wave` in its pair
+
+  // the slabs of a head, and neighbouring heads, one behind another on one XCD
+  const unsigned wg = workgroup(), at = wg / kXcdCount;
+  const unsigned unit = at / (unsigned)slabs * kXcdCount + wg % kXcdCount;
+  const int slab = (int)(at % (unsigned)slabs);
+  if (unit >= (unsigned)a.rows.B * (unsigned)a.H) return;
+  const int b = (int)(unit / (unsigned)a.H), h = (int)(unit % (unsigned)a.H), kh = h / (a.H / a.Hk);
+  const bool ok = starts_ok(a.rows, lane);
+  if (a.status && h == 0 && slab == 0 && threadIdx.x == 0) a.status[b] = ok ? SLA_OK : SLA_ERR_LENGTH;
+  if (!ok) return;
+  const int start = __builtin_amdgcn_readfirstlane(a.rows.start[b]);
+  const int len = __builtin_amdgcn_readfirstlane(a.rows.start[b + 1]) - start;
+  const int chunks = (len + kChunk - 1) / kChunk;
+  const size_t slot0 = (size_t)(start / kChunk) + b;
+
+  int col[NT];  // this lane's columns as an operand's row
+#pragma unroll
+  for (int n = 0; n < NT; ++n) col[n] = slab * 16 * NT + (NT == 1 ? r : 32 * (n / 2) + 8 * (r / 4) + 4 * (n % 2) + r % 4);
+
+  f32x4 H[kTiles][NT];
+#pragma unroll
+  for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        H[m][n][i] = a.state && col[n] < a.dv
+                         ? a.state[((size_t)unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] : 0.f;
+
+  // per-lane offsets inside a chunk
+  const uint32_t k_off = (uint32_t)(tile_row(wave, r) * a.k_stride * w) + 8 * g * w;
+  const uint32_t q_off = (uint32_t)(tile_row(wave, r) * a.q_stride * w) + 8 * g * w;
+  uint32_t v_off[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+    v_off[n] = col[n] < a.dv ? (uint32_t)(tile_row(wave, 4 * g) * a.v_stride * w) + col[n] * w : kNowhere;
+
+  auto rows_rsrc = [&](const void *p, int64_t stride, size_t first, int width, int chunk) {
+    const int left = min(kChunk, len - chunk * kChunk);  // rows of this chunk, none behind the last
+    const int64_t row = start + (int64_t)(left > 0 ? chunk : 0) * kChunk;
+    return make_rsrc(static_cast<const T *>(p) + row * stride + first, left > 0 ? (uint32_t)(((left - 1) * stride + width) * w) : 0u);
+  };
+  Frag<F32, 1> kf[kKs], qf[kKs], key[kTiles][2];
+  Frag<F32, kStatePlanes> ts[2];
+  Frag<F32, kOutPlanes> to[2];
+  uint32_t vr[NT][4];
+  f32x4 gr;      // decays of the rows 4 g + i
+  float gq, gc;  // of the row r, of the whole chunk
+  auto load_k = [&](int c) {
+    const rsrc_t rs = rows_rsrc(a.k, a.k_stride, (size_t)kh * DK, DK, c);
+#pragma unroll
+    for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+      for (int j = 0; j < kKeyPieces; ++j) reinterpret_cast<u32x4 *>(&kf[ks])[j] = buf_load16(rs, k_off + 32 * w * ks + 16 * j, 0);
+  };
+  auto load_q = [&](int c) {
+    const rsrc_t rs = rows_rsrc(a.q, a.q_stride, (size_t)kh * DK, DK, c);
+#pragma unroll
+    for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+      for (int j = 0; j < kKeyPieces; ++j) reinterpret_cast<u32x4 *>(&qf[ks])[j] = buf_load16(rs, q_off + 32 * w * ks + 16 * j, 0);
+  };
+  auto load_v = [&](int c) {
+    const rsrc_t rs = rows_rsrc(a.v, a.v_stride, (size_t)h * a.dv, a.dv, c);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t o = v_off[n] == kNowhere ? kNowhere : v_off[n] + (uint32_t)(i * a.v_stride * w);
+        vr[n][i] = F32 ? __builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, kPolicyDefault)
+                       : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rs, o, 0, kPolicyDefault) << 16;
+      }
+  };
+  const int t0 = first_frag(wave);
+  auto slot_of = [&](int c) { return slot0 + min(c, chunks - 1); };
+  auto load_decay = [&](int c) {
+    const float *d = reinterpret_cast<const float *>(space.head(slot_of(c), h) + space.kToState + space.kToOut);
+    gr = *reinterpret_cast<const f32x4 *>(d + tile_row(wave, 4 * g));
+    gq = d[tile_row(wave, r)];
+    gc = d[kChunk - 1];
+  };
+  auto load_matrices = [&](int c) {
+    const unsigned char *p = space.head(slot_of(c), h);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+      if (ks <= wave / 2) {
+        ts[ks] = get_frag<F32, kStatePlanes>(p + (size_t)(t0 + ks) * kPiecesOf<F32, kStatePlanes> * space.kPiece, lane);
+        to[ks] = get_frag<F32, kOutPlanes>(p + space.kToState + (size_t)(t0 + ks) * kPiecesOf<F32, kOutPlanes> * space.kPiece, lane);
+      }
+  };
+  auto load_keys = [&](int c) {
+    const unsigned char *p = space.keys(slot_of(c), kh);
+#pragma unroll
+    for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+        key[m][ks] = get_frag<F32, 1>(p + (size_t)((wave + 4 * m) * 2 + ks) * kKeyPieces * space.kPiece, lane);
+  };
+  auto put_state = [&] {
+#pragma unroll
+    for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        put_half<F32>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
+  };
+
+  if (chunks > 0) {
+    load_decay(0);
+    if (DELTA) load_k(0);
+    load_v(0);
+    load_q(0);
+    load_matrices(0);
+    load_keys(0);
+  }
+  for (int c = 0; c < chunks; ++c) {
+    put_state();
+    lds_barrier();
+    f32x4 acc[NT], o[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const Frag<F32, kStatePlanes> hf = get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane);
+        if (DELTA) acc[n] = mma<1, kStatePlanes>(kf[ks], hf, acc[n]);
+        o[n] = mma<kOutPlanes, 1>(hf, qf[ks], o[n]);
+      }
+    if (DELTA) load_k(c + 1);
+    load_q(c + 1);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      f32x4 rv;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rv[i] = DELTA ? __builtin_fmaf(-gr[i], acc[n][i], __uint_as_float(vr[n][i])) : __uint_as_float(vr[n][i]);
+      put_half<F32>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, rv);
+      o[n] *= gq;
+    }
+    const float whole = gc;
+    load_v(c + 1);
+    load_decay(c + 1);
+    lds_barrier();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+      if (ks <= wave / 2)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const Frag<F32, kStatePlanes> rf = get_frag<F32, kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane);
+          acc[n] = mma<kStatePlanes, kStatePlanes>(ts[ks], rf, acc[n]);
+          o[n] = mma<kOutPlanes, kOutPlanes>(rf, to[ks], o[n]);
+        }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) put_half<F32>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, acc[n]);
+    load_matrices(c + 1);
+    lds_barrier();
+#pragma unroll
+    for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) H[m][n] *= whole;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const Frag<F32, kStatePlanes> uf = get_frag<F32, kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
+#pragma unroll
+        for (int m = 0; m < kTiles; ++m) H[m][n] = mma<1, kStatePlanes>(key[m][ks], uf, H[m][n]);
+      }
+    load_keys(c + 1);
+    // lane: token tile_row(wave, r), columns 4 g + i of each tile
+    const int left = min(kChunk, len - c * kChunk), row = tile_row(wave, r);
+    if (row < left) {
+      T *out = static_cast<T *>(a.out) + ((size_t)(start + c * kChunk + row) * a.H + h) * a.dv;
+      if constexpr (NT == 1) {
+        const int at = slab * 16 + 4 * g;
+        if (at < a.dv)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (F32) out[at + i] = o[0][i];
+            else out[at + i].bits = (uint16_t)pack_bf16(o[0][i], 0.f);
+          }
+      } else {
+#pragma unroll
+        for (int n = 0; n < NT; n += 2) {
+          const int at = slab * 16 * NT + 16 * n + 8 * g;
+          const float x[8] = {o[n][0], o[n][1], o[n][2], o[n][3], o[n + 1][0], o[n + 1][1], o[n + 1][2], o[n + 1][3]};
+          if (at < a.dv) store8(out + at, x);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (col[n] < a.dv) a.state_out[((size_t)unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] = H[m][n][i];
+}
+
+// lets a kernel have more than 64 KiB of LDS
+template <typename K>
+hipError_t allow_lds(K kernel, size_t bytes) {
+  if (bytes <= (64u << 10)) return hipSuccess;
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+template <bool F32, int DK, bool DELTA>
+hipError_t launch_family(const PrefillArgs &a, hipStream_t s) {
+  constexpr int NT = 2;
+  using M = MatricesLds<F32, DK>;
+  using L = StateLds<F32, DK, NT>;
+  const auto first = matrices_kernel<F32, DK, DELTA>;
+  const auto second = state_kernel<F32, DK, NT, DELTA>;
+  hipError_t e = allow_lds(first, sizeof(M));
+  if (e == hipSuccess) e = allow_lds(second, L::kBytes);
+  if (e != hipSuccess) return e;
+  if (a.rows.tokens > 0) {
+    hipLaunchKernelGGL(first, grid_of((uint64_t)chunk_slots<kChunk>(a.rows) * a.H), dim3(kThreads), sizeof(M), s, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const int slabs = (a.dv + 16 * NT - 1) / (16 * NT);
+  const uint64_t units = ((uint64_t)a.rows.B * a.H + kXcdCount - 1) / kXcdCount * kXcdCount;
+  hipLaunchKernelGGL(second, grid_of(units * slabs), dim3(kThreads), L::kBytes, s, a, slabs);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+template <bool F32, int DK>
+hipError_t launch_chunks(const PrefillArgs &a, hipStream_t s) {
+  return a.family == SLA_FAMILY_DECAY ? launch_family<F32, DK, false>(a, s) : launch_family<F32, DK, true>(a, s);
+}
+
+template hipError_t launch_chunks<SLA_CHUNK_F32, SLA_CHUNK_DK>(const PrefillArgs &a, hipStream_t s);
+
+}  // namespace sla

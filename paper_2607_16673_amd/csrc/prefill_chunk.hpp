@@ -1,0 +1,114 @@
+// prefill_chunk.hpp -- what the two kernels of the chunked recurrence share: the
+// order of a chunk's tokens in matrix operands, those operands' types, and the
+// workspace in which the first leaves them for the second.
+//
+// Every matrix instruction here is v_mfma_f32_16x16x32_bf16 or eight
+// v_mfma_f32_16x16x4_f32 in a row.  Of an operand, lane l = 16 g + r holds row (or
+// column) r and the 8 inner indices 32 ks + 8 g + e, e = 0..7, 8 neighbouring
+// values; of a result, lane l holds column r of the rows 4 g + i, i = 0..3.  So
+// that a result can be the next product's operand in the lane where it is, the
+// 16-row tile 2 ks + h of 64 tokens (or of d_k) has as its row 4 g + i the index
+//     32 ks + 8 g + 4 h + i:
+// a pair of tiles then gives each lane its 8 neighbouring indices.
+#pragma once
+
+#include "prompt_device.hpp"
+
+namespace sla {
+
+constexpr int kChunk = 64;  // tokens of a chunk: four row tiles, one to a wave
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+
+// index of row `r` of tile `t`
+__host__ __device__ constexpr int tile_row(int t, int r) { return 32 * (t / 2) + 8 * (r / 4) + 4 * (t % 2) + r % 4; }
+
+// An operand: N bf16 planes whose sum it is (8 bits of the value each), or
+// fp32 values.
+template <bool F32, int N>
+struct Frag {
+  bf16x8 p[N];
+};
+template <int N>
+struct Frag<true, N> {
+  f32x4 p[2];
+};
+// 16-byte pieces of a lane
+template <bool F32, int N>
+constexpr int kPiecesOf = F32 ? 2 : N;
+
+// c + a b of the first NA and NB planes, products of 2^-8 max(NA, NB) and less
+// of the whole left out, small ones first.
+template <int NA, int NB, int N, int M>
+__device__ __forceinline__ f32x4 mma(const Frag<false, N> &a, const Frag<false, M> &b, f32x4 c) {
+  constexpr int kMost = (NA > NB ? NA : NB) - 1;
+#pragma unroll
+  for (int s = kMost; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+      if (s - i >= 0 && s - i < NB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], c, 0, 0, 0);
+  return c;
+}
+template <int NA, int NB, int N, int M>
+__device__ __forceinline__ f32x4 mma(const Frag<true, N> &a, const Frag<true, M> &b, f32x4 c) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.p[e / 4][e % 4], b.p[e / 4][e % 4], c, 0, 0, 0);
+  return c;
+}
+
+// The bf16 planes of 4 values, each the nearest to what the ones before leave.
+template <int N>
+__device__ __forceinline__ void split4(const float (&x)[4], uint2 (&p)[N]) {
+  float r[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    p[n] = make_uint2(pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3]));
+    if (n + 1 < N) {
+      r[0] -= __uint_as_float(p[n].x << 16);
+      r[1] -= __uint_as_float(p[n].x & 0xffff0000u);
+      r[2] -= __uint_as_float(p[n].y << 16);
+      r[3] -= __uint_as_float(p[n].y & 0xffff0000u);
+    }
+  }
+}
+
+// Planes of the two correction matrices: the one that makes the state, and the
+// one that makes outputs, which are rounded to bf16.
+constexpr int kStatePlanes = 3, kOutPlanes = 2;
+
+// Row tile t of the lower triangular 64 x 64 matrices has the inner 32s ks <= t / 2.
+__host__ __device__ constexpr int first_frag(int t) { return t < 2 ? t : 2 * t - 2; }
+constexpr int kTriFrags = 6;
+
+// What the first kernel leaves, operand by operand, 16 bytes a lane:
+//   for every (slot, head): to_state, to_out [6][pieces][64 lanes], decay [64] fp32;
+//   for every (slot, key head): keys [d_k / 16][2][pieces][64 lanes], K^T.
+template <bool F32, int DK>
+struct ChunkSpace {
+  static constexpr size_t kPiece = 64 * 16;
+  static constexpr size_t kToState = kTriFrags * kPiecesOf<F32, kStatePlanes> * kPiece;
+  static constexpr size_t kToOut = kTriFrags * kPiecesOf<F32, kOutPlanes> * kPiece;
+  static constexpr size_t kHead = kToState + kToOut + kChunk * 4;
+  static constexpr size_t kKeys = DK / 16 * 2 * kPiecesOf<F32, 1> * kPiece;
+
+  unsigned char *base;
+  size_t slots;
+  int H, Hk;
+
+  __host__ __device__ size_t bytes() const { return slots * (H * kHead + Hk * kKeys); }
+  __device__ unsigned char *head(size_t slot, int h) const { return base + (slot * H + h) * kHead; }
+  __device__ unsigned char *keys(size_t slot, int kh) const { return base + slots * H * kHead + (slot * Hk + kh) * kKeys; }
+};
+
+template <bool F32, int DK>
+__host__ __device__ inline ChunkSpace<F32, DK> chunk_space(const PrefillArgs &a) {
+  return {static_cast<unsigned char *>(a.workspace), (size_t)chunk_slots<kChunk>(a.rows), a.H, a.Hk};
+}
+
+// Each returns hipSuccess or the launch error (specialised in prefill_chunk.hip's units).
+template <bool F32, int DK>
+hipError_t launch_chunks(const PrefillArgs &a, hipStream_t s);
+
+}  // namespace sla

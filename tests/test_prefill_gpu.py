@@ -64,18 +64,19 @@ def test_rows_of_no_sequence_are_neither_read_nor_written(before, behind, dtype)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("what", ["q", "k", "v", "beta"])
 def test_neighbours_are_untouched_by_bad_values(what, bad):
-    p = Prompt([37, 70, 90], dv=32)
+    """A bad value spoils its sequence from its chunk of 64 tokens on, and nothing else."""
+    p = Prompt([37, 170, 90], dv=32)
     clean = p.run()
     want = p.exact()
-    getattr(p, what)[p.starts[1] + 5] = bad
+    getattr(p, what)[p.starts[1] + 70] = bad
     out, state, status = p.run()
     torch.cuda.synchronize()
     assert status.eq(0).all()
     for b in (0, 2):
         rows = slice(p.starts[b], p.starts[b + 1])
         assert torch.equal(out[rows], clean[0][rows]) and torch.equal(state[b], clean[1][b])
-    # tokens in front of the bad one, in its own sequence too
-    close(out[p.starts[1]:p.starts[1] + 5], want[0][p.starts[1]:p.starts[1] + 5])
+    first = slice(p.starts[1], p.starts[1] + 64)
+    close(out[first], want[0][first])
 
 
 def test_the_past_does_not_see_the_future():
