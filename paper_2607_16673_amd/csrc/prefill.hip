@@ -19,12 +19,6 @@ constexpr int kThreads = 256;
 constexpr int kCols = 64;   // columns of a workgroup
 constexpr int kStage = 16;  // tokens staged at a time
 
-__device__ __forceinline__ void store4(bf16 *p, const float (&x)[4]) {
-  *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-}
-__device__ __forceinline__ void store4(float *p, const float (&x)[4]) {
-  *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-}
 __device__ __forceinline__ void load4(const float *p, float (&x)[4]) { load_f32(p, x); }
 __device__ __forceinline__ void load4(const bf16 *p, float (&x)[4]) {
   const uint2 w = *reinterpret_cast<const uint2 *>(p);

@@ -332,14 +332,34 @@ __device__ __forceinline__ u32x4 buf_load16(rsrc_t r, uint32_t voff, uint32_t so
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, kPolicyDefault));
 }
 
+// Reads of operands from LDS run `AHEAD` operands in front of the `FRAGS` ones'
+// products: R reads and M matrix instructions each.
+template <int AHEAD, int R, int M, int FRAGS>
+__device__ __forceinline__ void pace() {
+  constexpr int kFirst = AHEAD < FRAGS ? AHEAD : FRAGS;
+  __builtin_amdgcn_sched_group_barrier(0x100, R * kFirst, 0);
+#pragma unroll
+  for (int f = 0; f < FRAGS; ++f) {
+    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+    if (f + kFirst < FRAGS) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  }
+}
+
+// matrix instructions of one product of N planes
+template <bool F32, int N>
+constexpr int kMfma = F32 ? 8 : N;
+constexpr int kAhead = 4;  // operands
+
 constexpr uint32_t kNowhere = 0x7fffffffu;  // an offset past any chunk's rows: reads give 0, writes are dropped
 
 template <bool F32, int DK, int NT, bool DELTA>
-__global__ __launch_bounds__(kThreads) void state_kernel(PrefillArgs a, int slabs) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void state_kernel(PrefillArgs a, int slabs) {
   using T = typename std::conditional<F32, float, bf16>::type;
   using L = StateLds<F32, DK, NT>;
   constexpr int kKs = DK / 32, kTiles = DK / 64, w = sizeof(T);
   constexpr int kKeyPieces = kPiecesOf<F32, 1>;
+  constexpr bool kHold = kKs * NT * L::kPieces <= 24;  // the state's operands all in registers at once
+  using Piece = typename Frag<F32, 1>::Piece;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   unsigned char *const lds_h = lds, *const lds_r = lds + L::kStateFrags * L::kFrag, *const lds_u = lds_r + L::kRowFrags * L::kFrag;
   const ChunkSpace<F32, DK> space = chunk_space<F32, DK>(a);
@@ -383,160 +403,212 @@ __global__ __launch_bounds__(kThreads) void state_kernel(PrefillArgs a, int slab
   for (int n = 0; n < NT; ++n)
     v_off[n] = col[n] < a.dv ? (uint32_t)(tile_row(wave, 4 * g) * a.v_stride * w) + col[n] * w : kNowhere;
 
-  auto rows_rsrc = [&](const void *p, int64_t stride, size_t first, int width, int chunk) {
-    const int left = min(kChunk, len - chunk * kChunk);  // rows of this chunk, none behind the last
-    const int64_t row = start + (int64_t)(left > 0 ? chunk : 0) * kChunk;
-    return make_rsrc(static_cast<const T *>(p) + row * stride + first, left > 0 ? (uint32_t)(((left - 1) * stride + width) * w) : 0u);
+  T *out = static_cast<T *>(a.out) + ((size_t)(start + tile_row(wave, r)) * a.H + h) * a.dv + slab * 16 * NT + (NT == 1 ? 4 : 8) * g;
+  const size_t out_step = (size_t)kChunk * a.H * a.dv;
+  // What a chunk reads, as descriptors that move on by a constant from chunk to
+  // chunk.  Past the sequence's last row and last chunk they read zeros, without a
+  // branch and without memory.
+  const int last = chunks - 1, tail = len - last * kChunk;
+  auto sized = [&](int c, uint32_t whole, uint32_t part) { return c < last ? whole : c == last ? part : 0u; };
+  struct Rows {
+    const unsigned char *at;
+    int64_t step;
+    uint32_t whole, part;
   };
+  auto rows_of = [&](const void *p, int64_t stride, size_t first, int width) {
+    return Rows{reinterpret_cast<const unsigned char *>(static_cast<const T *>(p) + start * stride + first), kChunk * stride * w,
+                (uint32_t)((kChunk - 1) * (int)stride + width) * w, (uint32_t)((tail - 1) * (int)stride + width) * w};
+  };
+  Rows k_rows = rows_of(a.k, a.k_stride, (size_t)kh * DK, DK), q_rows = rows_of(a.q, a.q_stride, (size_t)kh * DK, DK),
+       v_rows = rows_of(a.v, a.v_stride, (size_t)h * a.dv, a.dv);
+  const unsigned char *head_at = space.head(slot0, h), *keys_at = space.keys(slot0, kh);
+  const size_t head_step = (size_t)a.H * space.kHead, keys_step = (size_t)a.Hk * space.kKeys;
+
   Frag<F32, 1> kf[kKs], qf[kKs], key[kTiles][2];
   Frag<F32, kStatePlanes> ts[2];
   Frag<F32, kOutPlanes> to[2];
   uint32_t vr[NT][4];
   f32x4 gr;      // decays of the rows 4 g + i
   float gq, gc;  // of the row r, of the whole chunk
+  auto piece = [](rsrc_t rs, uint32_t voff, uint32_t soff) { return __builtin_bit_cast(Piece, buf_load16(rs, voff, soff)); };
   auto load_k = [&](int c) {
-    const rsrc_t rs = rows_rsrc(a.k, a.k_stride, (size_t)kh * DK, DK, c);
+    const rsrc_t rs = make_rsrc(k_rows.at, sized(c, k_rows.whole, k_rows.part));
+    k_rows.at += k_rows.step;
 #pragma unroll
     for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
-      for (int j = 0; j < kKeyPieces; ++j) reinterpret_cast<u32x4 *>(&kf[ks])[j] = buf_load16(rs, k_off + 32 * w * ks + 16 * j, 0);
+      for (int j = 0; j < kKeyPieces; ++j) kf[ks].p[j] = piece(rs, k_off + 32 * w * ks + 16 * j, 0);
   };
   auto load_q = [&](int c) {
-    const rsrc_t rs = rows_rsrc(a.q, a.q_stride, (size_t)kh * DK, DK, c);
+    const rsrc_t rs = make_rsrc(q_rows.at, sized(c, q_rows.whole, q_rows.part));
+    q_rows.at += q_rows.step;
 #pragma unroll
     for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
-      for (int j = 0; j < kKeyPieces; ++j) reinterpret_cast<u32x4 *>(&qf[ks])[j] = buf_load16(rs, q_off + 32 * w * ks + 16 * j, 0);
+      for (int j = 0; j < kKeyPieces; ++j) qf[ks].p[j] = piece(rs, q_off + 32 * w * ks + 16 * j, 0);
   };
   auto load_v = [&](int c) {
-    const rsrc_t rs = rows_rsrc(a.v, a.v_stride, (size_t)h * a.dv, a.dv, c);
+    const rsrc_t rs = make_rsrc(v_rows.at, sized(c, v_rows.whole, v_rows.part));
+    v_rows.at += v_rows.step;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t o = v_off[n] == kNowhere ? kNowhere : v_off[n] + (uint32_t)(i * a.v_stride * w);
-        vr[n][i] = F32 ? __builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, kPolicyDefault)
-                       : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rs, o, 0, kPolicyDefault) << 16;
-      }
+      for (int i = 0; i < 4; ++i)
+        vr[n][i] = F32 ? __builtin_amdgcn_raw_buffer_load_b32(rs, v_off[n], (uint32_t)(i * (int)a.v_stride * w), kPolicyDefault)
+                       : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rs, v_off[n], (uint32_t)(i * (int)a.v_stride * w), kPolicyDefault);
   };
+  // the matrices and decays of the head; row tiles 0 and 1 have no second inner 32
   const int t0 = first_frag(wave);
-  auto slot_of = [&](int c) { return slot0 + min(c, chunks - 1); };
-  auto load_decay = [&](int c) {
-    const float *d = reinterpret_cast<const float *>(space.head(slot_of(c), h) + space.kToState + space.kToOut);
-    gr = *reinterpret_cast<const f32x4 *>(d + tile_row(wave, 4 * g));
-    gq = d[tile_row(wave, r)];
-    gc = d[kChunk - 1];
-  };
   auto load_matrices = [&](int c) {
-    const unsigned char *p = space.head(slot_of(c), h);
+    const uint32_t bytes = c <= last ? (uint32_t)space.kHead : 0u;
+    const rsrc_t rs = make_rsrc(head_at, bytes), more = make_rsrc(head_at, wave < 2 ? 0u : bytes);
+    head_at += head_step;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-      if (ks <= wave / 2) {
-        ts[ks] = get_frag<F32, kStatePlanes>(p + (size_t)(t0 + ks) * kPiecesOf<F32, kStatePlanes> * space.kPiece, lane);
-        to[ks] = get_frag<F32, kOutPlanes>(p + space.kToState + (size_t)(t0 + ks) * kPiecesOf<F32, kOutPlanes> * space.kPiece, lane);
-      }
+    for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+      for (int j = 0; j < kPiecesOf<F32, kStatePlanes>; ++j)
+        ts[ks].p[j] = piece(ks ? more : rs, lane * 16 + j * space.kPiece, (t0 + ks) * kPiecesOf<F32, kStatePlanes> * space.kPiece);
+#pragma unroll
+      for (int j = 0; j < kPiecesOf<F32, kOutPlanes>; ++j)
+        to[ks].p[j] = piece(ks ? more : rs, lane * 16 + j * space.kPiece,
+                            space.kToState + (t0 + ks) * kPiecesOf<F32, kOutPlanes> * space.kPiece);
+    }
+    constexpr uint32_t kDecay = space.kToState + space.kToOut;
+    gr = __builtin_bit_cast(f32x4, buf_load16(rs, tile_row(wave, 4 * g) * 4, kDecay));
+    gq = buf_load_f32<kPolicyDefault>(rs, tile_row(wave, r) * 4, kDecay);
+    gc = buf_load_f32<kPolicyDefault>(rs, (kChunk - 1) * 4, kDecay);
   };
   auto load_keys = [&](int c) {
-    const unsigned char *p = space.keys(slot_of(c), kh);
+    const rsrc_t rs = make_rsrc(keys_at, c <= last ? (uint32_t)space.kKeys : 0u);
+    keys_at += keys_step;
 #pragma unroll
     for (int m = 0; m < kTiles; ++m)
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
-        key[m][ks] = get_frag<F32, 1>(p + (size_t)((wave + 4 * m) * 2 + ks) * kKeyPieces * space.kPiece, lane);
+#pragma unroll
+        for (int j = 0; j < kKeyPieces; ++j)
+          key[m][ks].p[j] = piece(rs, lane * 16 + j * space.kPiece, ((wave + 4 * m) * 2 + ks) * kKeyPieces * space.kPiece);
   };
-  auto put_state = [&] {
+  auto put_state = [&](int m) {
 #pragma unroll
-    for (int m = 0; m < kTiles; ++m)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        put_half<F32>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
+    for (int n = 0; n < NT; ++n)
+      put_half<F32>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
   };
 
   if (chunks > 0) {
-    load_decay(0);
     if (DELTA) load_k(0);
     load_v(0);
     load_q(0);
     load_matrices(0);
     load_keys(0);
   }
+#pragma unroll
+  for (int m = 0; m < kTiles; ++m) put_state(m);
   for (int c = 0; c < chunks; ++c) {
-    put_state();
     lds_barrier();
+    // K H, which the rest waits for, and Q H
     f32x4 acc[NT], o[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n] = o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto state_frag = [&](int ks, int n) { return get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane); };
+    if constexpr (DELTA && kHold) {
+      Frag<F32, kStatePlanes> hf[kKs][NT];
 #pragma unroll
-    for (int ks = 0; ks < kKs; ++ks)
+      for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const Frag<F32, kStatePlanes> hf = get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane);
-        if (DELTA) acc[n] = mma<1, kStatePlanes>(kf[ks], hf, acc[n]);
-        o[n] = mma<kOutPlanes, 1>(hf, qf[ks], o[n]);
-      }
-    if (DELTA) load_k(c + 1);
-    load_q(c + 1);
+        for (int n = 0; n < NT; ++n) hf[ks][n] = state_frag(ks, n);
+#pragma unroll
+      for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[n] = mma<1, kStatePlanes>(kf[ks], hf[ks][n], acc[n]);
+      pace<kKs * NT, L::kPieces, kMfma<F32, 3>, kKs * NT>();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[n] = mma<kOutPlanes, 1>(hf[ks][n], qf[ks], o[n]);
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const Frag<F32, kStatePlanes> hf = state_frag(ks, n);
+          if (DELTA) acc[n] = mma<1, kStatePlanes>(kf[ks], hf, acc[n]);
+          o[n] = mma<kOutPlanes, 1>(hf, qf[ks], o[n]);
+        }
+      pace<kAhead, L::kPieces, (DELTA ? kMfma<F32, 3> : 0) + kMfma<F32, 2>, kKs * NT>();
+      __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       f32x4 rv;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) rv[i] = DELTA ? __builtin_fmaf(-gr[i], acc[n][i], __uint_as_float(vr[n][i])) : __uint_as_float(vr[n][i]);
+      for (int i = 0; i < 4; ++i) {
+        const float v = __uint_as_float(F32 ? vr[n][i] : vr[n][i] << 16);
+        rv[i] = DELTA ? __builtin_fmaf(-gr[i], acc[n][i], v) : v;
+      }
       put_half<F32>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, rv);
-      o[n] *= gq;
     }
-    const float whole = gc;
+    if (DELTA) load_k(c + 1);
     load_v(c + 1);
-    load_decay(c + 1);
+    load_q(c + 1);
     lds_barrier();
+    // the corrected values, which the state waits for, and the outputs' share of R
+    Frag<F32, kStatePlanes> rf[2][NT];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) rf[ks][n] = get_frag<F32, kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane);
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
-      if (ks <= wave / 2)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const Frag<F32, kStatePlanes> rf = get_frag<F32, kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane);
-          acc[n] = mma<kStatePlanes, kStatePlanes>(ts[ks], rf, acc[n]);
-          o[n] = mma<kOutPlanes, kOutPlanes>(rf, to[ks], o[n]);
-        }
+      for (int n = 0; n < NT; ++n) acc[n] = mma<kStatePlanes, kStatePlanes>(ts[ks], rf[ks][n], acc[n]);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) put_half<F32>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, acc[n]);
-    load_matrices(c + 1);
-    lds_barrier();
-#pragma unroll
-    for (int m = 0; m < kTiles; ++m)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) H[m][n] *= whole;
+    for (int n = 0; n < NT; ++n) o[n] *= gq;
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const Frag<F32, kStatePlanes> uf = get_frag<F32, kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
+      for (int n = 0; n < NT; ++n) o[n] = mma<kOutPlanes, kOutPlanes>(rf[ks][n], to[ks], o[n]);
 #pragma unroll
-        for (int m = 0; m < kTiles; ++m) H[m][n] = mma<1, kStatePlanes>(key[m][ks], uf, H[m][n]);
-      }
+    for (int n = 0; n < NT; ++n) put_half<F32>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, acc[n]);
+    const float whole = gc;
+    load_matrices(c + 1);
+    lds_barrier();
+    // the next state
+    Frag<F32, kStatePlanes> uf[2][NT];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) uf[ks][n] = get_frag<F32, kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
+#pragma unroll
+    for (int m = 0; m < kTiles; ++m) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) H[m][n] *= whole;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) H[m][n] = mma<1, kStatePlanes>(key[m][ks], uf[ks][n], H[m][n]);
+    }
+#pragma unroll
+    for (int m = 0; m < kTiles; ++m) put_state(m);
     load_keys(c + 1);
     // lane: token tile_row(wave, r), columns 4 g + i of each tile
-    const int left = min(kChunk, len - c * kChunk), row = tile_row(wave, r);
-    if (row < left) {
-      T *out = static_cast<T *>(a.out) + ((size_t)(start + c * kChunk + row) * a.H + h) * a.dv;
+    if (tile_row(wave, r) < len - c * kChunk) {
       if constexpr (NT == 1) {
-        const int at = slab * 16 + 4 * g;
-        if (at < a.dv)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (F32) out[at + i] = o[0][i];
-            else out[at + i].bits = (uint16_t)pack_bf16(o[0][i], 0.f);
-          }
+        const float x[4] = {o[0][0], o[0][1], o[0][2], o[0][3]};
+        store4(out, x);
       } else {
 #pragma unroll
         for (int n = 0; n < NT; n += 2) {
-          const int at = slab * 16 * NT + 16 * n + 8 * g;
           const float x[8] = {o[n][0], o[n][1], o[n][2], o[n][3], o[n + 1][0], o[n + 1][1], o[n + 1][2], o[n + 1][3]};
-          if (at < a.dv) store8(out + at, x);
+          if (slab * 16 * NT + 16 * n + 8 * g < a.dv) store8(out + 16 * n, x);
         }
       }
     }
+    out += out_step;
   }
 #pragma unroll
   for (int m = 0; m < kTiles; ++m)
@@ -554,25 +626,30 @@ hipError_t allow_lds(K kernel, size_t bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <bool F32, int DK, bool DELTA>
-hipError_t launch_family(const PrefillArgs &a, hipStream_t s) {
-  constexpr int NT = 2;
-  using M = MatricesLds<F32, DK>;
+template <bool F32, int DK, int NT, bool DELTA>
+hipError_t launch_states(const PrefillArgs &a, hipStream_t s) {
   using L = StateLds<F32, DK, NT>;
-  const auto first = matrices_kernel<F32, DK, DELTA>;
   const auto second = state_kernel<F32, DK, NT, DELTA>;
-  hipError_t e = allow_lds(first, sizeof(M));
-  if (e == hipSuccess) e = allow_lds(second, L::kBytes);
+  const hipError_t e = allow_lds(second, L::kBytes);
   if (e != hipSuccess) return e;
-  if (a.rows.tokens > 0) {
-    hipLaunchKernelGGL(first, grid_of((uint64_t)chunk_slots<kChunk>(a.rows) * a.H), dim3(kThreads), sizeof(M), s, a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   const int slabs = (a.dv + 16 * NT - 1) / (16 * NT);
   const uint64_t units = ((uint64_t)a.rows.B * a.H + kXcdCount - 1) / kXcdCount * kXcdCount;
   hipLaunchKernelGGL(second, grid_of(units * slabs), dim3(kThreads), L::kBytes, s, a, slabs);
   return hipGetLastError();
+}
+
+template <bool F32, int DK, bool DELTA>
+hipError_t launch_family(const PrefillArgs &a, hipStream_t s) {
+  using M = MatricesLds<F32, DK>;
+  const auto first = matrices_kernel<F32, DK, DELTA>;
+  hipError_t e = allow_lds(first, sizeof(M));
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(first, grid_of((uint64_t)chunk_slots<kChunk>(a.rows) * a.H), dim3(kThreads), sizeof(M), s, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  // 16 columns of a state to a workgroup where 32 leave half of the CUs without one
+  const int64_t wide = (int64_t)a.rows.B * a.H * ((a.dv + 31) / 32);
+  return wide <= device_cus() / 2 ? launch_states<F32, DK, 1, DELTA>(a, s) : launch_states<F32, DK, 2, DELTA>(a, s);
 }
 
 }  // namespace

@@ -25,15 +25,16 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 // index of row `r` of tile `t`
 __host__ __device__ constexpr int tile_row(int t, int r) { return 32 * (t / 2) + 8 * (r / 4) + 4 * (t % 2) + r % 4; }
 
-// An operand: N bf16 planes whose sum it is (8 bits of the value each), or
-// fp32 values.
+// An operand: N bf16 planes, 8 bits of the values each, or fp32 values.
 template <bool F32, int N>
 struct Frag {
-  bf16x8 p[N];
+  using Piece = bf16x8;
+  Piece p[N];
 };
 template <int N>
 struct Frag<true, N> {
-  f32x4 p[2];
+  using Piece = f32x4;
+  Piece p[2];
 };
 // 16-byte pieces of a lane
 template <bool F32, int N>
@@ -58,19 +59,20 @@ __device__ __forceinline__ f32x4 mma(const Frag<true, N> &a, const Frag<true, M>
   return c;
 }
 
-// The bf16 planes of 4 values, each the nearest to what the ones before leave.
+// The bf16 planes of 4 values: the leading 8 bits of each, the next 8, the last
+// 8 (cut, not rounded: three planes are the value itself, and a mask and a
+// subtraction cost less than a conversion).
 template <int N>
 __device__ __forceinline__ void split4(const float (&x)[4], uint2 (&p)[N]) {
-  float r[4] = {x[0], x[1], x[2], x[3]};
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(x[i]);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    p[n] = make_uint2(pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3]));
-    if (n + 1 < N) {
-      r[0] -= __uint_as_float(p[n].x << 16);
-      r[1] -= __uint_as_float(p[n].x & 0xffff0000u);
-      r[2] -= __uint_as_float(p[n].y << 16);
-      r[3] -= __uint_as_float(p[n].y & 0xffff0000u);
-    }
+    p[n] = make_uint2(__builtin_amdgcn_perm(r[1], r[0], 0x07060302u), __builtin_amdgcn_perm(r[3], r[2], 0x07060302u));
+    if (n + 1 < N)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) - __uint_as_float(r[i] & 0xffff0000u));
   }
 }
 

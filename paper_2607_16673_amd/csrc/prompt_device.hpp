@@ -7,6 +7,13 @@
 
 namespace sla {
 
+__device__ __forceinline__ void store4(bf16 *p, const float (&x)[4]) {
+  *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+}
+__device__ __forceinline__ void store4(float *p, const float (&x)[4]) {
+  *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+}
+
 // Whether the starts are in order and inside the rows (wave-uniform).  Every
 // wave looks at all of them: the loads are independent, 64 sequences at a time.
 __device__ __forceinline__ bool starts_ok(const PackedRows &r, int lane) {

@@ -196,14 +196,18 @@ def test_equal_calls_give_equal_bits_in_any_batch(lens):
     out, state, _ = p.run()
     again = p.run()
     assert torch.equal(out, again[0]) and torch.equal(state, again[1])
+    want = p.exact()
     for b, n in enumerate(lens):  # the same number of rows, the others of no sequence
         one = Prompt(lens, heads=2, dv=48)
         one.B, one.state = 1, p.state[b:b + 1].clone()
         one.start = torch.tensor(p.starts[b:b + 2].tolist(), dtype=torch.int32, device="cuda")
         o, s, _ = one.run()
         rows = slice(p.starts[b], p.starts[b + 1])
-        close(o[rows], f64(out[rows]))
-        close(s, f64(state[b:b + 1]))
+        if max(lens) > 1:
+            assert torch.equal(o[rows], out[rows]) and torch.equal(s, state[b:b + 1])
+        else:  # single tokens alone take the kernel of long sequences: each is a rounding from the exact value
+            close(o[rows], want[0][rows])
+            close(s, want[1][b:b + 1])
 
 
 @pytest.mark.parametrize("lens", [[100, 64, 3], [1] * 20])
