@@ -258,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       x[e] = DELTA ? s.x[row * kPitch + at + e] * s.beta[at + e] * rest : at + e == row ? rest : 0.f;
-      p[e] = s.p[row * kPitch + at + e];
+      p[e] = s.p[(16 * wave + r) * kPitch + at + e];  // outputs keep the order of their tokens
     }
     store_frag<F32, kStatePlanes>(head + (size_t)f * kPiecesOf<F32, kStatePlanes> * space.kPiece, lane, x);
     store_frag<F32, kOutPlanes>(head + space.kToState + (size_t)f * kPiecesOf<F32, kOutPlanes> * space.kPiece, lane, p);
@@ -267,6 +267,15 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
     reinterpret_cast<float *>(head + space.kToState + space.kToOut)[threadIdx.x] = s.decay[threadIdx.x];
   if (h % group == 0) {
     unsigned char *keys = space.keys(slot, kh);
+#pragma unroll
+    for (int ks = 0; ks < DK / 32; ++ks)
+#pragma unroll
+      for (int j = 0; j < kPiecesOf<F32, 1>; ++j) {
+        const size_t at = (((size_t)wave * (DK / 32) + ks) * kPiecesOf<F32, 1> + j) * space.kPiece + lane * 16;
+        *reinterpret_cast<u32x4 *>(keys + space.kRows + at) =
+            reinterpret_cast<const u32x4 *>(s.k + row * L::kKeyPitch + 32 * ks + 8 * g)[j];
+        *reinterpret_cast<u32x4 *>(keys + 2 * space.kRows + at) = reinterpret_cast<const u32x4 *>(&q[ks])[j];
+      }
     for (int f = wave; f < DK / 16 * 2; f += kThreads / kWave) {
       const T *from = s.k + (32 * (f % 2) + 8 * g) * L::kKeyPitch + tile_row(f / 2, r);
       unsigned char *to = keys + (size_t)f * kPiecesOf<F32, 1> * space.kPiece;
@@ -288,11 +297,12 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
 
 // ----------------------------------------------------------- second kernel
 // One workgroup = one (sequence, head) and 16 NT columns of its state, which stay
-// in the accumulators of its four waves from the first chunk to the last: wave w
-// has the row tiles w, w + 4, .. of d_k.  Of a chunk it has the token tile w.  The
-// state, R and the corrected values pass through LDS as operands, three barriers
-// a chunk; what comes from memory is asked for as soon as the chunk before has
-// used its registers.
+// in the accumulators of four waves from the first chunk to the last: wave w has
+// the row tiles w, w + 4, .. of d_k and the token tile w.  These waves do what the
+// next state waits for: K H, R, the corrected values, the update.  Four others, one
+// on the same SIMD as each, make the outputs from the same operands in LDS, in the
+// time the first ones wait for one another: three barriers a chunk.  What comes
+// from memory is asked for as soon as the chunk before has used its registers.
 //
 // Columns: lane r of column tile n has the column 32 (n / 2) + 8 (r / 4) + 4 (n % 2)
 // + r % 4 of the slab, so that an output tile, made transposed, gives each lane 8
@@ -323,13 +333,13 @@ template <bool F32, int N>
 __device__ __forceinline__ Frag<F32, N> get_frag(const unsigned char *frag, int lane) {
   Frag<F32, N> f;
 #pragma unroll
-  for (int n = 0; n < kPiecesOf<F32, N>; ++n)
-    reinterpret_cast<u32x4 *>(&f)[n] = *reinterpret_cast<const u32x4 *>(frag + (n * kWave + lane) * 16);
+  for (int n = 0; n < kPiecesOf<F32, N>; ++n) f.p[n] = *reinterpret_cast<const typename Frag<F32, N>::Piece *>(frag + (n * kWave + lane) * 16);
   return f;
 }
 
-__device__ __forceinline__ u32x4 buf_load16(rsrc_t r, uint32_t voff, uint32_t soff) {
-  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, kPolicyDefault));
+template <typename P>
+__device__ __forceinline__ P load_piece(rsrc_t r, uint32_t voff, uint32_t soff) {
+  return __builtin_bit_cast(P, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, kPolicyDefault));
 }
 
 // Reads of operands from LDS run `AHEAD` operands in front of the `FRAGS` ones'
@@ -348,22 +358,37 @@ __device__ __forceinline__ void pace() {
 // matrix instructions of one product of N planes
 template <bool F32, int N>
 constexpr int kMfma = F32 ? 8 : N;
-constexpr int kAhead = 4;  // operands
 
-constexpr uint32_t kNowhere = 0x7fffffffu;  // an offset past any chunk's rows: reads give 0, writes are dropped
+constexpr int kStateThreads = 512;
+constexpr uint32_t kNowhere = 0x40000000u;  // an offset past any chunk's rows: reads give 0
+
+// What a chunk reads of a tensor, as a descriptor that moves on by a constant from
+// chunk to chunk.  Past the sequence's last row and last chunk it reads zeros,
+// without a branch and without memory.
+struct ChunkRows {
+  const unsigned char *at;
+  int64_t step;
+  uint32_t whole, part;
+  int last;
+  __device__ __forceinline__ rsrc_t next(int c) {
+    const rsrc_t r = make_rsrc(at, c < last ? whole : c == last ? part : 0u);
+    at += step;
+    return r;
+  }
+};
 
 template <bool F32, int DK, int NT, bool DELTA>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void state_kernel(PrefillArgs a, int slabs) {
+__global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void state_kernel(PrefillArgs a, int slabs) {
   using T = typename std::conditional<F32, float, bf16>::type;
   using L = StateLds<F32, DK, NT>;
-  constexpr int kKs = DK / 32, kTiles = DK / 64, w = sizeof(T);
-  constexpr int kKeyPieces = kPiecesOf<F32, 1>;
-  constexpr bool kHold = kKs * NT * L::kPieces <= 24;  // the state's operands all in registers at once
   using Piece = typename Frag<F32, 1>::Piece;
+  constexpr int kKs = DK / 32, kTiles = DK / 64, w = sizeof(T);
+  constexpr int kKeyPieces = kPiecesOf<F32, 1>, kStatePieces = kPiecesOf<F32, kStatePlanes>, kOutPieces = kPiecesOf<F32, kOutPlanes>;
+  constexpr int kAhead = 24 / (NT * L::kPieces);  // of the state's operands read in front of their products
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   unsigned char *const lds_h = lds, *const lds_r = lds + L::kStateFrags * L::kFrag, *const lds_u = lds_r + L::kRowFrags * L::kFrag;
   const ChunkSpace<F32, DK> space = chunk_space<F32, DK>(a);
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int lane = threadIdx.x % kWave, role = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wave = role % 4;
   const int g = lane / 16, r = lane % 16;
   const int half = wave % 2;  // of the token tile `wave` in its pair
 
@@ -378,245 +403,240 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (!ok) return;
   const int start = __builtin_amdgcn_readfirstlane(a.rows.start[b]);
   const int len = __builtin_amdgcn_readfirstlane(a.rows.start[b + 1]) - start;
-  const int chunks = (len + kChunk - 1) / kChunk;
+  const int chunks = (len + kChunk - 1) / kChunk, last = chunks - 1, tail = len - last * kChunk;
   const size_t slot0 = (size_t)(start / kChunk) + b;
-
-  int col[NT];  // this lane's columns as an operand's row
-#pragma unroll
-  for (int n = 0; n < NT; ++n) col[n] = slab * 16 * NT + (NT == 1 ? r : 32 * (n / 2) + 8 * (r / 4) + 4 * (n % 2) + r % 4);
-
-  f32x4 H[kTiles][NT];
-#pragma unroll
-  for (int m = 0; m < kTiles; ++m)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        H[m][n][i] = a.state && col[n] < a.dv
-                         ? a.state[((size_t)unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] : 0.f;
-
-  // per-lane offsets inside a chunk
-  const uint32_t k_off = (uint32_t)(tile_row(wave, r) * a.k_stride * w) + 8 * g * w;
-  const uint32_t q_off = (uint32_t)(tile_row(wave, r) * a.q_stride * w) + 8 * g * w;
-  uint32_t v_off[NT];
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-    v_off[n] = col[n] < a.dv ? (uint32_t)(tile_row(wave, 4 * g) * a.v_stride * w) + col[n] * w : kNowhere;
-
-  T *out = static_cast<T *>(a.out) + ((size_t)(start + tile_row(wave, r)) * a.H + h) * a.dv + slab * 16 * NT + (NT == 1 ? 4 : 8) * g;
-  const size_t out_step = (size_t)kChunk * a.H * a.dv;
-  // What a chunk reads, as descriptors that move on by a constant from chunk to
-  // chunk.  Past the sequence's last row and last chunk they read zeros, without a
-  // branch and without memory.
-  const int last = chunks - 1, tail = len - last * kChunk;
-  auto sized = [&](int c, uint32_t whole, uint32_t part) { return c < last ? whole : c == last ? part : 0u; };
-  struct Rows {
-    const unsigned char *at;
-    int64_t step;
-    uint32_t whole, part;
-  };
   auto rows_of = [&](const void *p, int64_t stride, size_t first, int width) {
-    return Rows{reinterpret_cast<const unsigned char *>(static_cast<const T *>(p) + start * stride + first), kChunk * stride * w,
-                (uint32_t)((kChunk - 1) * (int)stride + width) * w, (uint32_t)((tail - 1) * (int)stride + width) * w};
+    return ChunkRows{reinterpret_cast<const unsigned char *>(static_cast<const T *>(p) + start * stride + first),
+                     kChunk * stride * w, (uint32_t)((kChunk - 1) * (int)stride + width) * w,
+                     (uint32_t)((tail - 1) * (int)stride + width) * w, last};
   };
-  Rows k_rows = rows_of(a.k, a.k_stride, (size_t)kh * DK, DK), q_rows = rows_of(a.q, a.q_stride, (size_t)kh * DK, DK),
-       v_rows = rows_of(a.v, a.v_stride, (size_t)h * a.dv, a.dv);
-  const unsigned char *head_at = space.head(slot0, h), *keys_at = space.keys(slot0, kh);
-  const size_t head_step = (size_t)a.H * space.kHead, keys_step = (size_t)a.Hk * space.kKeys;
-
-  Frag<F32, 1> kf[kKs], qf[kKs], key[kTiles][2];
-  Frag<F32, kStatePlanes> ts[2];
-  Frag<F32, kOutPlanes> to[2];
-  uint32_t vr[NT][4];
-  f32x4 gr;      // decays of the rows 4 g + i
-  float gq, gc;  // of the row r, of the whole chunk
-  auto piece = [](rsrc_t rs, uint32_t voff, uint32_t soff) { return __builtin_bit_cast(Piece, buf_load16(rs, voff, soff)); };
-  auto load_k = [&](int c) {
-    const rsrc_t rs = make_rsrc(k_rows.at, sized(c, k_rows.whole, k_rows.part));
-    k_rows.at += k_rows.step;
-#pragma unroll
-    for (int ks = 0; ks < kKs; ++ks)
-#pragma unroll
-      for (int j = 0; j < kKeyPieces; ++j) kf[ks].p[j] = piece(rs, k_off + 32 * w * ks + 16 * j, 0);
-  };
-  auto load_q = [&](int c) {
-    const rsrc_t rs = make_rsrc(q_rows.at, sized(c, q_rows.whole, q_rows.part));
-    q_rows.at += q_rows.step;
-#pragma unroll
-    for (int ks = 0; ks < kKs; ++ks)
-#pragma unroll
-      for (int j = 0; j < kKeyPieces; ++j) qf[ks].p[j] = piece(rs, q_off + 32 * w * ks + 16 * j, 0);
-  };
-  auto load_v = [&](int c) {
-    const rsrc_t rs = make_rsrc(v_rows.at, sized(c, v_rows.whole, v_rows.part));
-    v_rows.at += v_rows.step;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        vr[n][i] = F32 ? __builtin_amdgcn_raw_buffer_load_b32(rs, v_off[n], (uint32_t)(i * (int)a.v_stride * w), kPolicyDefault)
-                       : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rs, v_off[n], (uint32_t)(i * (int)a.v_stride * w), kPolicyDefault);
-  };
-  // the matrices and decays of the head; row tiles 0 and 1 have no second inner 32
+  ChunkRows head_rows = {space.head(slot0, h), (int64_t)(a.H * space.kHead), (uint32_t)space.kHead, (uint32_t)space.kHead, last};
+  ChunkRows key_rows = {space.keys(slot0, kh), (int64_t)(a.Hk * space.kKeys), (uint32_t)space.kKeys, (uint32_t)space.kKeys, last};
   const int t0 = first_frag(wave);
-  auto load_matrices = [&](int c) {
-    const uint32_t bytes = c <= last ? (uint32_t)space.kHead : 0u;
-    const rsrc_t rs = make_rsrc(head_at, bytes), more = make_rsrc(head_at, wave < 2 ? 0u : bytes);
-    head_at += head_step;
+  constexpr uint32_t kDecay = ChunkSpace<F32, DK>::kToState + ChunkSpace<F32, DK>::kToOut;
+  constexpr uint32_t kPiece = ChunkSpace<F32, DK>::kPiece, kRows = ChunkSpace<F32, DK>::kRows;
+
+  if (role < 4) {
+    int col[NT];  // this lane's columns as an operand's row
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-#pragma unroll
-      for (int j = 0; j < kPiecesOf<F32, kStatePlanes>; ++j)
-        ts[ks].p[j] = piece(ks ? more : rs, lane * 16 + j * space.kPiece, (t0 + ks) * kPiecesOf<F32, kStatePlanes> * space.kPiece);
-#pragma unroll
-      for (int j = 0; j < kPiecesOf<F32, kOutPlanes>; ++j)
-        to[ks].p[j] = piece(ks ? more : rs, lane * 16 + j * space.kPiece,
-                            space.kToState + (t0 + ks) * kPiecesOf<F32, kOutPlanes> * space.kPiece);
-    }
-    constexpr uint32_t kDecay = space.kToState + space.kToOut;
-    gr = __builtin_bit_cast(f32x4, buf_load16(rs, tile_row(wave, 4 * g) * 4, kDecay));
-    gq = buf_load_f32<kPolicyDefault>(rs, tile_row(wave, r) * 4, kDecay);
-    gc = buf_load_f32<kPolicyDefault>(rs, (kChunk - 1) * 4, kDecay);
-  };
-  auto load_keys = [&](int c) {
-    const rsrc_t rs = make_rsrc(keys_at, c <= last ? (uint32_t)space.kKeys : 0u);
-    keys_at += keys_step;
+    for (int n = 0; n < NT; ++n) col[n] = slab * 16 * NT + (NT == 1 ? r : 32 * (n / 2) + 8 * (r / 4) + 4 * (n % 2) + r % 4);
+    f32x4 H[kTiles][NT];
 #pragma unroll
     for (int m = 0; m < kTiles; ++m)
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int j = 0; j < kKeyPieces; ++j)
-          key[m][ks].p[j] = piece(rs, lane * 16 + j * space.kPiece, ((wave + 4 * m) * 2 + ks) * kKeyPieces * space.kPiece);
-  };
-  auto put_state = [&](int m) {
+        for (int i = 0; i < 4; ++i)
+          H[m][n][i] = a.state && col[n] < a.dv
+                           ? a.state[((size_t)unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] : 0.f;
+
+    ChunkRows v_rows = rows_of(a.v, a.v_stride, (size_t)h * a.dv, a.dv);
+    uint32_t v_off[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-      put_half<F32>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
-  };
-
-  if (chunks > 0) {
-    if (DELTA) load_k(0);
-    load_v(0);
-    load_q(0);
-    load_matrices(0);
-    load_keys(0);
-  }
-#pragma unroll
-  for (int m = 0; m < kTiles; ++m) put_state(m);
-  for (int c = 0; c < chunks; ++c) {
-    lds_barrier();
-    // K H, which the rest waits for, and Q H
-    f32x4 acc[NT], o[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n] = o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto state_frag = [&](int ks, int n) { return get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane); };
-    if constexpr (DELTA && kHold) {
-      Frag<F32, kStatePlanes> hf[kKs][NT];
+      v_off[n] = col[n] < a.dv ? (uint32_t)(tile_row(wave, 4 * g) * (int)a.v_stride + col[n]) * w : kNowhere;
+    Frag<F32, 1> kf[kKs], key[kTiles][2];
+    Frag<F32, kStatePlanes> ts[2];
+    uint32_t vr[NT][4];
+    f32x4 gr;  // decays of the rows 4 g + i
+    float gc;  // of the whole chunk
+    auto load_k = [&](rsrc_t rs) {
 #pragma unroll
       for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) hf[ks][n] = state_frag(ks, n);
+        for (int j = 0; j < kKeyPieces; ++j)
+          kf[ks].p[j] = load_piece<Piece>(rs, lane * 16 + j * kPiece, kRows + (wave * kKs + ks) * kKeyPieces * kPiece);
+    };
+    auto load_v = [&](int c) {
+      const rsrc_t rs = v_rows.next(c);
 #pragma unroll
-      for (int ks = 0; ks < kKs; ++ks)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[n] = mma<1, kStatePlanes>(kf[ks], hf[ks][n], acc[n]);
-      pace<kKs * NT, L::kPieces, kMfma<F32, 3>, kKs * NT>();
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int ks = 0; ks < kKs; ++ks)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) o[n] = mma<kOutPlanes, 1>(hf[ks][n], qf[ks], o[n]);
-    } else {
-#pragma unroll
-      for (int ks = 0; ks < kKs; ++ks)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const Frag<F32, kStatePlanes> hf = state_frag(ks, n);
-          if (DELTA) acc[n] = mma<1, kStatePlanes>(kf[ks], hf, acc[n]);
-          o[n] = mma<kOutPlanes, 1>(hf, qf[ks], o[n]);
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t row = (uint32_t)(i * (int)a.v_stride * w);
+          vr[n][i] = F32 ? __builtin_amdgcn_raw_buffer_load_b32(rs, v_off[n], row, kPolicyDefault)
+                         : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rs, v_off[n], row, kPolicyDefault);
         }
-      pace<kAhead, L::kPieces, (DELTA ? kMfma<F32, 3> : 0) + kMfma<F32, 2>, kKs * NT>();
-      __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      f32x4 rv;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float v = __uint_as_float(F32 ? vr[n][i] : vr[n][i] << 16);
-        rv[i] = DELTA ? __builtin_fmaf(-gr[i], acc[n][i], v) : v;
-      }
-      put_half<F32>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, rv);
-    }
-    if (DELTA) load_k(c + 1);
-    load_v(c + 1);
-    load_q(c + 1);
-    lds_barrier();
-    // the corrected values, which the state waits for, and the outputs' share of R
-    Frag<F32, kStatePlanes> rf[2][NT];
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) rf[ks][n] = get_frag<F32, kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) acc[n] = mma<kStatePlanes, kStatePlanes>(ts[ks], rf[ks][n], acc[n]);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) o[n] *= gq;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) o[n] = mma<kOutPlanes, kOutPlanes>(rf[ks][n], to[ks], o[n]);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) put_half<F32>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, acc[n]);
-    const float whole = gc;
-    load_matrices(c + 1);
-    lds_barrier();
-    // the next state
-    Frag<F32, kStatePlanes> uf[2][NT];
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) uf[ks][n] = get_frag<F32, kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
-#pragma unroll
-    for (int m = 0; m < kTiles; ++m) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) H[m][n] *= whole;
+    };
+    auto load_decay = [&](rsrc_t rs) {
+      gr = load_piece<f32x4>(rs, tile_row(wave, 4 * g) * 4, kDecay);
+      gc = buf_load_f32<kPolicyDefault>(rs, (kChunk - 1) * 4, kDecay);
+    };
+    rsrc_t head = head_rows.next(0), keys = key_rows.next(0);
+    auto load_matrix = [&] {  // row tiles 0 and 1 have no second inner 32
+      const rsrc_t more = wave < 2 ? make_rsrc(head_rows.at, 0u) : head;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) H[m][n] = mma<1, kStatePlanes>(key[m][ks], uf[ks][n], H[m][n]);
+        for (int j = 0; j < kStatePieces; ++j)
+          ts[ks].p[j] = load_piece<Piece>(ks ? more : head, lane * 16 + j * kPiece, (t0 + ks) * kStatePieces * kPiece);
+    };
+    auto load_keys = [&](rsrc_t rs) {
+#pragma unroll
+      for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int j = 0; j < kKeyPieces; ++j)
+            key[m][ks].p[j] = load_piece<Piece>(rs, lane * 16 + j * kPiece, ((wave + 4 * m) * 2 + ks) * kKeyPieces * kPiece);
+    };
+    auto put_state = [&](int m) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        put_half<F32>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
+    };
+
+    __builtin_amdgcn_s_setprio(2);
+    if (chunks > 0) {
+      if (DELTA) load_k(keys);
+      load_v(0);
+      load_decay(head);
+      load_matrix();
+      load_keys(keys);
     }
 #pragma unroll
     for (int m = 0; m < kTiles; ++m) put_state(m);
-    load_keys(c + 1);
-    // lane: token tile_row(wave, r), columns 4 g + i of each tile
-    if (tile_row(wave, r) < len - c * kChunk) {
-      if constexpr (NT == 1) {
-        const float x[4] = {o[0][0], o[0][1], o[0][2], o[0][3]};
-        store4(out, x);
-      } else {
+    for (int c = 0; c < chunks; ++c) {
+      lds_barrier();
+      f32x4 acc[NT];
+      if constexpr (DELTA) {
 #pragma unroll
-        for (int n = 0; n < NT; n += 2) {
-          const float x[8] = {o[n][0], o[n][1], o[n][2], o[n][3], o[n + 1][0], o[n + 1][1], o[n + 1][2], o[n + 1][3]};
-          if (slab * 16 * NT + 16 * n + 8 * g < a.dv) store8(out + 16 * n, x);
+        for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            acc[n] = mma<1, kStatePlanes>(kf[ks], get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane), acc[n]);
+        pace<kAhead, L::kPieces, kMfma<F32, 3>, kKs * NT>();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        f32x4 rv;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float v = __uint_as_float(F32 ? vr[n][i] : vr[n][i] << 16);
+          rv[i] = DELTA ? __builtin_fmaf(-gr[i], acc[n][i], v) : v;
+        }
+        put_half<F32>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, rv);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const float whole = gc;
+      head = head_rows.next(c + 1);
+      keys = key_rows.next(c + 1);
+      if (DELTA) load_k(keys);
+      load_v(c + 1);
+      load_decay(head);
+      lds_barrier();
+      Frag<F32, kStatePlanes> rf[2][NT];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) rf[ks][n] = get_frag<F32, kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[n] = mma<kStatePlanes, kStatePlanes>(ts[ks], rf[ks][n], acc[n]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) put_half<F32>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, acc[n]);
+      __builtin_amdgcn_sched_barrier(0);
+      load_matrix();
+      lds_barrier();
+      Frag<F32, kStatePlanes> uf[2][NT];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) uf[ks][n] = get_frag<F32, kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
+#pragma unroll
+      for (int m = 0; m < kTiles; ++m) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) H[m][n] *= whole;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) H[m][n] = mma<1, kStatePlanes>(key[m][ks], uf[ks][n], H[m][n]);
+      }
+#pragma unroll
+      for (int m = 0; m < kTiles; ++m) put_state(m);
+      load_keys(keys);
+    }
+#pragma unroll
+    for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (col[n] < a.dv) a.state_out[((size_t)unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] = H[m][n][i];
+  } else {
+    // lane: token 16 wave + r, columns 4 g + i of each tile
+    const int token = 16 * wave + r;
+    T *out = static_cast<T *>(a.out) + ((size_t)(start + token) * a.H + h) * a.dv + slab * 16 * NT + (NT == 1 ? 4 : 8) * g;
+    const size_t out_step = (size_t)kChunk * a.H * a.dv;
+    Frag<F32, 1> qf[kKs];
+    Frag<F32, kOutPlanes> to[2];
+    float gq;  // decay of the token
+    auto load_q = [&](int c) {
+      const rsrc_t rs = key_rows.next(c);
+#pragma unroll
+      for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+        for (int j = 0; j < kKeyPieces; ++j)
+          qf[ks].p[j] = load_piece<Piece>(rs, lane * 16 + j * kPiece, 2 * kRows + (wave * kKs + ks) * kKeyPieces * kPiece);
+    };
+    auto load_matrix = [&](int c) {
+      const rsrc_t rs = head_rows.next(c), more = wave < 2 ? make_rsrc(head_rows.at, 0u) : rs;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int j = 0; j < kOutPieces; ++j)
+          to[ks].p[j] = load_piece<Piece>(ks ? more : rs, lane * 16 + j * kPiece,
+                                          ChunkSpace<F32, DK>::kToState + (t0 + ks) * kOutPieces * kPiece);
+      gq = buf_load_f32<kPolicyDefault>(rs, token * 4, kDecay);
+    };
+    if (chunks > 0) {
+      load_q(0);
+      load_matrix(0);
+    }
+    for (int c = 0; c < chunks; ++c) {
+      lds_barrier();
+      f32x4 o[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          o[n] = mma<kOutPlanes, 1>(get_frag<F32, kOutPlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane), qf[ks], o[n]);
+      pace<kAhead, kOutPieces, kMfma<F32, 2>, kKs * NT>();
+      __builtin_amdgcn_sched_barrier(0);
+      load_q(c + 1);
+      lds_barrier();
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[n] *= gq;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          o[n] = mma<kOutPlanes, kOutPlanes>(get_frag<F32, kOutPlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane), to[ks], o[n]);
+      lds_barrier();
+      load_matrix(c + 1);
+      if (token < len - c * kChunk) {
+        if constexpr (NT == 1) {
+          const float x[4] = {o[0][0], o[0][1], o[0][2], o[0][3]};
+          store4(out, x);
+        } else {
+#pragma unroll
+          for (int n = 0; n < NT; n += 2) {
+            const float x[8] = {o[n][0], o[n][1], o[n][2], o[n][3], o[n + 1][0], o[n + 1][1], o[n + 1][2], o[n + 1][3]};
+            if (slab * 16 * NT + 16 * n + 8 * g < a.dv) store8(out + 16 * n, x);
+          }
         }
       }
+      out += out_step;
     }
-    out += out_step;
   }
-#pragma unroll
-  for (int m = 0; m < kTiles; ++m)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (col[n] < a.dv) a.state_out[((size_t)unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] = H[m][n][i];
 }
 
 // lets a kernel have more than 64 KiB of LDS
@@ -634,7 +654,7 @@ hipError_t launch_states(const PrefillArgs &a, hipStream_t s) {
   if (e != hipSuccess) return e;
   const int slabs = (a.dv + 16 * NT - 1) / (16 * NT);
   const uint64_t units = ((uint64_t)a.rows.B * a.H + kXcdCount - 1) / kXcdCount * kXcdCount;
-  hipLaunchKernelGGL(second, grid_of(units * slabs), dim3(kThreads), L::kBytes, s, a, slabs);
+  hipLaunchKernelGGL(second, grid_of(units * slabs), dim3(kStateThreads), L::kBytes, s, a, slabs);
   return hipGetLastError();
 }
 

@@ -86,14 +86,19 @@ constexpr int kTriFrags = 6;
 
 // What the first kernel leaves, operand by operand, 16 bytes a lane:
 //   for every (slot, head): to_state, to_out [6][pieces][64 lanes], decay [64] fp32;
-//   for every (slot, key head): keys [d_k / 16][2][pieces][64 lanes], K^T.
+//   for every (slot, key head): K^T [d_k / 16][2][pieces][64 lanes], and K and Q
+//   [4][d_k / 32][pieces][64 lanes].  Keys and queries lie one token a row, often a
+//   power of two apart, so that a head's rows all fall to one channel of the L2; the
+//   workgroups of a head that read them chunk by chunk would wait there for one
+//   another (one sequence of 32768 tokens, 16 heads: 998 us against NNN).
 template <bool F32, int DK>
 struct ChunkSpace {
   static constexpr size_t kPiece = 64 * 16;
   static constexpr size_t kToState = kTriFrags * kPiecesOf<F32, kStatePlanes> * kPiece;
   static constexpr size_t kToOut = kTriFrags * kPiecesOf<F32, kOutPlanes> * kPiece;
   static constexpr size_t kHead = kToState + kToOut + kChunk * 4;
-  static constexpr size_t kKeys = DK / 16 * 2 * kPiecesOf<F32, 1> * kPiece;
+  static constexpr size_t kRows = 4 * (DK / 32) * kPiecesOf<F32, 1> * kPiece;  // of K, of Q, and of K^T
+  static constexpr size_t kKeys = 3 * kRows;
 
   unsigned char *base;
   size_t slots;
