@@ -4,12 +4,12 @@
 // With D_ij the product of the gates j + 1 .. i and G_i of those up to i (from
 // the chunk's start), H the state in front of it, Q, K, V its rows:
 //     X = (I + L)^-1,  L_ij = beta_i D_ij k_i . k_j  (j < i)
-//     R = V - G o (K H)
-//     out = G o (Q H) + [(D o Q K^T, lower) X beta] R
-//     H' = G_63 H + K^T [D_63 o X beta] R
-// The matrices in brackets do not depend on the state.  A first kernel makes them
-// for all chunks at once; a second walks each sequence's chunks in order.  Gates
-// are only multiplied: no logarithm, no quotient, so tiny ones do no harm.
+//     U = X beta (V - G o (K H))          (no delta rule: U = V)
+//     out = G o (Q H) + (D o Q K^T, lower) U
+//     H' = G_63 H + K^T (D_63 o U)
+// X beta and D o Q K^T do not depend on the state.  A first kernel makes them for
+// all chunks at once; a second walks each sequence's chunks in order.  Gates are
+// only multiplied: no logarithm, no quotient, so tiny ones do no harm.
 //
 // A sequence's NaN or infinity reaches all outputs of its chunk of 64 tokens, those
 // of earlier tokens in it included, and no other sequence.
@@ -39,7 +39,6 @@ struct MatricesLds {
   static constexpr int kKeyPitch = DK + 16 / (int)sizeof(T);
   T k[kChunk * kKeyPitch];
   float x[kChunk * kPitch];  // L, then X
-  float p[kChunk * kPitch];  // D o Q K^T, then times X beta
   float d[4][16][16];        // D inside the diagonal blocks
   float upto[kChunk];        // product of a block's gates up to i
   float behind[kChunk];      // product of a block's gates behind j
@@ -153,42 +152,76 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
   }
   lds_barrier();
 
-  // K K^T and Q K^T, decayed: row tile `wave`, column tiles up to it
+  unsigned char *const head = space.head(slot, h);
+  auto key_frag = [&](int row, int ks) {
+    Frag<F32, 1> f;
+#pragma unroll
+    for (int j = 0; j < kPiecesOf<F32, 1>; ++j)
+      f.p[j] = reinterpret_cast<const typename Frag<F32, 1>::Piece *>(s.k + row * L::kKeyPitch + 32 * ks + 8 * g)[j];
+    return f;
+  };
+  // Q K^T, decayed: the query tile `wave`, transposed, so that the lane has its
+  // operand: query 16 wave + r, keys 32 ks + 8 g + e
   {
+    const int query = 16 * wave + r;
+    const float upto = s.upto[query];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      if (ks > wave / 2) continue;
+      const int block = 2 * ks + g / 2;  // of the lane's keys
+      float mid = upto;                  // ... times the blocks between
+      if (wave - block > 1) mid *= s.total[block + 1];
+      if (wave - block > 2) mid *= s.total[block + 2];
+      float p[8];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        Sum<2> sum;
+#pragma unroll
+        for (int i = 0; i < DK / 32; ++i) {
+          if constexpr (F32) {
+            sum.template add<1, 1>(key_frag(tile_row(2 * ks + t, r), i), q[i]);
+          } else {
+            sum.s[i % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key_frag(tile_row(2 * ks + t, r), i).p[0], q[i].p[0], sum.s[i % 2], 0, 0, 0);
+          }
+        }
+        const f32x4 qk = sum.total();
+        const int key = 32 * ks + 8 * g + 4 * t;
+        const f32x4 behind = *reinterpret_cast<const f32x4 *>(s.behind + key);
+        const f32x4 same = *reinterpret_cast<const f32x4 *>(&s.d[wave][r][key % 16]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[4 * t + i] = key + i > query ? 0.f : qk[i] * (block == wave ? same[i] : mid * behind[i]);
+      }
+      store_frag<F32, kOutPlanes>(head + space.kSolve + (size_t)(first_frag(wave) + ks) * kPiecesOf<F32, kOutPlanes> * space.kPiece, lane, p);
+    }
+  }
+  if (threadIdx.x < kChunk) {
+    reinterpret_cast<float *>(head + space.kDecay)[threadIdx.x] = s.decay[threadIdx.x];
+    reinterpret_cast<float *>(head + space.kRest)[threadIdx.x] = s.rest[threadIdx.x];
+  }
+
+  if constexpr (DELTA) {
+    // L: the row tile 3 - wave, which evens out the waves' products
+    const int rt = 3 - wave;
     Frag<F32, 1> kr[DK / 32];
 #pragma unroll
-    for (int ks = 0; ks < DK / 32; ++ks)
-#pragma unroll
-      for (int j = 0; j < kPiecesOf<F32, 1>; ++j)
-        reinterpret_cast<u32x4 *>(&kr[ks])[j] =
-            reinterpret_cast<const u32x4 *>(s.k + (16 * wave + r) * L::kKeyPitch + 32 * ks + 8 * g)[j];
+    for (int ks = 0; ks < DK / 32; ++ks) kr[ks] = key_frag(16 * rt + r, ks);
     float mid = 1.f;  // product of the blocks between the columns' and the rows'
-    for (int t = wave; t >= 0; --t) {
-      f32x4 kk = {0.f, 0.f, 0.f, 0.f}, qk = {0.f, 0.f, 0.f, 0.f};
+    for (int t = rt; t >= 0; --t) {
+      Sum<1> sum;
 #pragma unroll
-      for (int ks = 0; ks < DK / 32; ++ks) {
-        Frag<F32, 1> col;
-#pragma unroll
-        for (int j = 0; j < kPiecesOf<F32, 1>; ++j)
-          reinterpret_cast<u32x4 *>(&col)[j] =
-              reinterpret_cast<const u32x4 *>(s.k + (16 * t + r) * L::kKeyPitch + 32 * ks + 8 * g)[j];
-        if (DELTA) kk = mma<1, 1>(kr[ks], col, kk);
-        qk = mma<1, 1>(q[ks], col, qk);
-      }
+      for (int ks = 0; ks < DK / 32; ++ks) sum.template add<1, 1>(kr[ks], key_frag(16 * t + r, ks));
+      const f32x4 kk = sum.total();
       const float behind = s.behind[16 * t + r] * mid;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int row = 16 * wave + 4 * g + i;
-        const float d = t == wave ? s.d[wave][4 * g + i][r] : s.upto[row] * behind;
-        if (DELTA) s.x[row * kPitch + 16 * t + r] = t == wave && 4 * g + i <= r ? 0.f : s.beta[row] * d * kk[i];
-        s.p[row * kPitch + 16 * t + r] = t == wave && 4 * g + i < r ? 0.f : d * qk[i];
+        const int row = 16 * rt + 4 * g + i;
+        const float d = t == rt ? s.d[rt][4 * g + i][r] : s.upto[row] * behind;
+        s.x[row * kPitch + 16 * t + r] = t == rt && 4 * g + i <= r ? 0.f : s.beta[row] * d * kk[i];
       }
-      if (t < wave) mid *= s.total[t];
+      if (t < rt) mid *= s.total[t];
     }
-    if (wave % 2 == 0) {  // right of the diagonal: the operands reach there
-      block_store(s.x, wave, wave + 1, g, r, f32x4{0.f, 0.f, 0.f, 0.f});
-      block_store(s.p, wave, wave + 1, g, r, f32x4{0.f, 0.f, 0.f, 0.f});
-    }
+    if (rt % 2 == 0)  // right of the diagonal: the operands reach there
+      block_store(s.x, rt, rt + 1, g, r, f32x4{0.f, 0.f, 0.f, 0.f});
   }
 
   if constexpr (DELTA) {
@@ -233,38 +266,15 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
                   -block_mma(block_a(s.x, 3, 3, g, r), y3, block_mma(block_a(s.x, 3, 2, g, r), y2, zero)));
     }
     lds_barrier();
-    f32x4 px[4];
+    // out: row tile `wave` as the second kernel's operand
+    for (int ks = 0; ks <= wave / 2; ++ks) {
+      const int at = 32 * ks + 8 * g;
+      float x[8];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      px[t] = zero;
-      if (t > wave) continue;
-      for (int m = t; m <= wave; ++m) px[t] = block_mma(block_a(s.p, wave, m, g, r), block_b(s.x, m, t, g, r), px[t]);
-      px[t] *= s.beta[16 * t + r];
+      for (int e = 0; e < 8; ++e) x[e] = s.x[tile_row(wave, r) * kPitch + at + e] * s.beta[at + e];
+      store_frag<F32, kStatePlanes>(head + (size_t)(first_frag(wave) + ks) * kPiecesOf<F32, kStatePlanes> * space.kPiece, lane, x);
     }
-    // a row tile's blocks have one reader and writer, its wave
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-      if (t <= wave) block_store(s.p, wave, t, g, r, px[t]);
   }
-  lds_barrier();
-
-  // out: row tile `wave` as the second kernel's operands
-  unsigned char *head = space.head(slot, h);
-  const int row = tile_row(wave, r);
-  const float rest = s.rest[row];
-  for (int ks = 0; ks <= wave / 2; ++ks) {
-    const int f = first_frag(wave) + ks, at = 32 * ks + 8 * g;
-    float x[8], p[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[e] = DELTA ? s.x[row * kPitch + at + e] * s.beta[at + e] * rest : at + e == row ? rest : 0.f;
-      p[e] = s.p[(16 * wave + r) * kPitch + at + e];  // outputs keep the order of their tokens
-    }
-    store_frag<F32, kStatePlanes>(head + (size_t)f * kPiecesOf<F32, kStatePlanes> * space.kPiece, lane, x);
-    store_frag<F32, kOutPlanes>(head + space.kToState + (size_t)f * kPiecesOf<F32, kOutPlanes> * space.kPiece, lane, p);
-  }
-  if (threadIdx.x < kChunk)
-    reinterpret_cast<float *>(head + space.kToState + space.kToOut)[threadIdx.x] = s.decay[threadIdx.x];
   if (h % group == 0) {
     unsigned char *keys = space.keys(slot, kh);
 #pragma unroll
@@ -273,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
       for (int j = 0; j < kPiecesOf<F32, 1>; ++j) {
         const size_t at = (((size_t)wave * (DK / 32) + ks) * kPiecesOf<F32, 1> + j) * space.kPiece + lane * 16;
         *reinterpret_cast<u32x4 *>(keys + space.kRows + at) =
-            reinterpret_cast<const u32x4 *>(s.k + row * L::kKeyPitch + 32 * ks + 8 * g)[j];
+            reinterpret_cast<const u32x4 *>(s.k + tile_row(wave, r) * L::kKeyPitch + 32 * ks + 8 * g)[j];
         *reinterpret_cast<u32x4 *>(keys + 2 * space.kRows + at) = reinterpret_cast<const u32x4 *>(&q[ks])[j];
       }
     for (int f = wave; f < DK / 16 * 2; f += kThreads / kWave) {
@@ -310,22 +320,24 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
 template <bool F32, int DK, int NT>
 struct StateLds {
   static constexpr int kPieces = kPiecesOf<F32, kStatePlanes>;
-  static constexpr size_t kFrag = (size_t)kPieces * kWave * 16;
+  static constexpr int kOutPieces = kPiecesOf<F32, kOutPlanes>;
+  static constexpr size_t kFrag = (size_t)kPieces * kWave * 16, kOutFrag = (size_t)kOutPieces * kWave * 16;
   static constexpr int kStateFrags = DK / 32 * NT, kRowFrags = 2 * NT;
-  static constexpr size_t kBytes = (kStateFrags + 2 * kRowFrags) * kFrag;
+  // H, V - G o (K H), D_63 o U, U
+  static constexpr size_t kBytes = (kStateFrags + 2 * kRowFrags) * kFrag + kRowFrags * kOutFrag;
 };
 
 // half `half` (4 of 8 values) of a lane's operand
-template <bool F32>
+template <bool F32, int N>
 __device__ __forceinline__ void put_half(unsigned char *frag, int half, int lane, f32x4 x) {
   if constexpr (F32) {
     *reinterpret_cast<f32x4 *>(frag + (half * kWave + lane) * 16) = x;
   } else {
     const float v[4] = {x[0], x[1], x[2], x[3]};
-    uint2 p[kStatePlanes];
+    uint2 p[N];
     split4(v, p);
 #pragma unroll
-    for (int n = 0; n < kStatePlanes; ++n) *reinterpret_cast<uint2 *>(frag + (n * kWave + lane) * 16 + 8 * half) = p[n];
+    for (int n = 0; n < N; ++n) *reinterpret_cast<uint2 *>(frag + (n * kWave + lane) * 16 + 8 * half) = p[n];
   }
 }
 
@@ -360,6 +372,9 @@ template <bool F32, int N>
 constexpr int kMfma = F32 ? 8 : N;
 
 constexpr int kStateThreads = 512;
+// of the state kernel: two workgroups to a CU where their registers hold the operands
+template <bool F32, int DK, int NT>
+constexpr int kWavesPerSimd = NT > 1 && DK <= (F32 ? 64 : 128) ? 4 : 2;
 constexpr uint32_t kNowhere = 0x40000000u;  // an offset past any chunk's rows: reads give 0
 
 // What a chunk reads of a tensor, as a descriptor that moves on by a constant from
@@ -378,15 +393,17 @@ struct ChunkRows {
 };
 
 template <bool F32, int DK, int NT, bool DELTA>
-__global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void state_kernel(PrefillArgs a, int slabs) {
+__global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<F32, DK, NT>, kWavesPerSimd<F32, DK, NT>))) void state_kernel(PrefillArgs a, int slabs) {
   using T = typename std::conditional<F32, float, bf16>::type;
   using L = StateLds<F32, DK, NT>;
   using Piece = typename Frag<F32, 1>::Piece;
   constexpr int kKs = DK / 32, kTiles = DK / 64, w = sizeof(T);
   constexpr int kKeyPieces = kPiecesOf<F32, 1>, kStatePieces = kPiecesOf<F32, kStatePlanes>, kOutPieces = kPiecesOf<F32, kOutPlanes>;
-  constexpr int kAhead = 24 / (NT * L::kPieces);  // of the state's operands read in front of their products
+  constexpr int kParts = NT == 1 ? (F32 ? 2 : 3) : 1, kOutParts = NT == 1 ? 2 : 1;
+  constexpr int kAhead = NT == 1 ? 8 : 2;  // of the state's operands read in front of their products
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  unsigned char *const lds_h = lds, *const lds_r = lds + L::kStateFrags * L::kFrag, *const lds_u = lds_r + L::kRowFrags * L::kFrag;
+  unsigned char *const lds_h = lds, *const lds_r = lds + L::kStateFrags * L::kFrag, *const lds_u = lds_r + L::kRowFrags * L::kFrag,
+                *const lds_o = lds_u + L::kRowFrags * L::kFrag;
   const ChunkSpace<F32, DK> space = chunk_space<F32, DK>(a);
   const int lane = threadIdx.x % kWave, role = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wave = role % 4;
   const int g = lane / 16, r = lane % 16;
@@ -413,7 +430,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(2
   ChunkRows head_rows = {space.head(slot0, h), (int64_t)(a.H * space.kHead), (uint32_t)space.kHead, (uint32_t)space.kHead, last};
   ChunkRows key_rows = {space.keys(slot0, kh), (int64_t)(a.Hk * space.kKeys), (uint32_t)space.kKeys, (uint32_t)space.kKeys, last};
   const int t0 = first_frag(wave);
-  constexpr uint32_t kDecay = ChunkSpace<F32, DK>::kToState + ChunkSpace<F32, DK>::kToOut;
+  constexpr uint32_t kDecay = ChunkSpace<F32, DK>::kDecay, kRest = ChunkSpace<F32, DK>::kRest;
   constexpr uint32_t kPiece = ChunkSpace<F32, DK>::kPiece, kRows = ChunkSpace<F32, DK>::kRows;
 
   if (role < 4) {
@@ -438,7 +455,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(2
     Frag<F32, 1> kf[kKs], key[kTiles][2];
     Frag<F32, kStatePlanes> ts[2];
     uint32_t vr[NT][4];
-    f32x4 gr;  // decays of the rows 4 g + i
+    f32x4 gr, gu;  // decays of the rows 4 g + i, and behind them
     float gc;  // of the whole chunk
     auto load_k = [&](rsrc_t rs) {
 #pragma unroll
@@ -459,7 +476,8 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(2
         }
     };
     auto load_decay = [&](rsrc_t rs) {
-      gr = load_piece<f32x4>(rs, tile_row(wave, 4 * g) * 4, kDecay);
+      if (DELTA) gr = load_piece<f32x4>(rs, tile_row(wave, 4 * g) * 4, kDecay);
+      gu = load_piece<f32x4>(rs, tile_row(wave, 4 * g) * 4, kRest);
       gc = buf_load_f32<kPolicyDefault>(rs, (kChunk - 1) * 4, kDecay);
     };
     rsrc_t head = head_rows.next(0), keys = key_rows.next(0);
@@ -483,7 +501,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(2
     auto put_state = [&](int m) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
-        put_half<F32>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
+        put_half<F32, kStatePlanes>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
     };
 
     __builtin_amdgcn_s_setprio(2);
@@ -491,76 +509,86 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(2
       if (DELTA) load_k(keys);
       load_v(0);
       load_decay(head);
-      load_matrix();
+      if (DELTA) load_matrix();
       load_keys(keys);
     }
 #pragma unroll
     for (int m = 0; m < kTiles; ++m) put_state(m);
     for (int c = 0; c < chunks; ++c) {
       lds_barrier();
-      f32x4 acc[NT];
+      f32x4 hk[NT];
       if constexpr (DELTA) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        Sum<kParts> sum[NT];
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            acc[n] = mma<1, kStatePlanes>(kf[ks], get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane), acc[n]);
+            sum[n].template add<1, kStatePlanes>(kf[ks], get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane));
         pace<kAhead, L::kPieces, kMfma<F32, 3>, kKs * NT>();
         __builtin_amdgcn_sched_barrier(0);
-      }
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        f32x4 rv;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float v = __uint_as_float(F32 ? vr[n][i] : vr[n][i] << 16);
-          rv[i] = DELTA ? __builtin_fmaf(-gr[i], acc[n][i], v) : v;
-        }
-        put_half<F32>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, rv);
+        for (int n = 0; n < NT; ++n) hk[n] = sum[n].total();
       }
-      __builtin_amdgcn_sched_barrier(0);
-      const float whole = gc;
       head = head_rows.next(c + 1);
       keys = key_rows.next(c + 1);
       if (DELTA) load_k(keys);
+      f32x4 u[NT];  // V - G o (K H), then U
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float v = __uint_as_float(F32 ? vr[n][i] : vr[n][i] << 16);
+          u[n][i] = DELTA ? __builtin_fmaf(-gr[i], hk[n][i], v) : v;
+        }
+        if (DELTA) put_half<F32, kStatePlanes>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, u[n]);
+      }
       load_v(c + 1);
-      load_decay(head);
-      lds_barrier();
-      Frag<F32, kStatePlanes> rf[2][NT];
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) rf[ks][n] = get_frag<F32, kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[n] = mma<kStatePlanes, kStatePlanes>(ts[ks], rf[ks][n], acc[n]);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) put_half<F32>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, acc[n]);
-      __builtin_amdgcn_sched_barrier(0);
-      load_matrix();
-      lds_barrier();
-      Frag<F32, kStatePlanes> uf[2][NT];
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) uf[ks][n] = get_frag<F32, kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
-#pragma unroll
-      for (int m = 0; m < kTiles; ++m) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) H[m][n] *= whole;
+      if constexpr (DELTA) {
+        lds_barrier();
+        Sum<kParts> sum[NT];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) H[m][n] = mma<1, kStatePlanes>(key[m][ks], uf[ks][n], H[m][n]);
+          for (int n = 0; n < NT; ++n)
+            sum[n].template add<kStatePlanes, kStatePlanes>(ts[ks], get_frag<F32, kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane));
+        pace<2, L::kPieces, F32 ? 8 : 6, 2 * NT>();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) u[n] = sum[n].total();
+        load_matrix();
       }
 #pragma unroll
-      for (int m = 0; m < kTiles; ++m) put_state(m);
+      for (int n = 0; n < NT; ++n) {
+        put_half<F32, kStatePlanes>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, gu * u[n]);
+        put_half<F32, kOutPlanes>(lds_o + (size_t)(wave / 2 * NT + n) * L::kOutFrag, half, lane, u[n]);
+      }
+      const float whole = gc;
+      load_decay(head);
+      lds_barrier();
+      {
+        Sum<kParts> next[kTiles][NT];
+#pragma unroll
+        for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) next[m][n].s[0] = H[m][n] * whole;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const Frag<F32, kStatePlanes> uf = get_frag<F32, kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
+#pragma unroll
+            for (int m = 0; m < kTiles; ++m) next[m][n].template add<1, kStatePlanes>(key[m][ks], uf);
+          }
+        pace<2, L::kPieces, kTiles * kMfma<F32, 3>, 2 * NT>();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) H[m][n] = next[m][n].total();
+      }
       load_keys(keys);
+#pragma unroll
+      for (int m = 0; m < kTiles; ++m) put_state(m);
     }
 #pragma unroll
     for (int m = 0; m < kTiles; ++m)
@@ -592,7 +620,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(2
 #pragma unroll
         for (int j = 0; j < kOutPieces; ++j)
           to[ks].p[j] = load_piece<Piece>(ks ? more : rs, lane * 16 + j * kPiece,
-                                          ChunkSpace<F32, DK>::kToState + (t0 + ks) * kOutPieces * kPiece);
+                                          ChunkSpace<F32, DK>::kSolve + (t0 + ks) * kOutPieces * kPiece);
       gq = buf_load_f32<kPolicyDefault>(rs, token * 4, kDecay);
     };
     if (chunks > 0) {
@@ -601,26 +629,29 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(2
     }
     for (int c = 0; c < chunks; ++c) {
       lds_barrier();
-      f32x4 o[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+      Sum<kOutParts> sum[NT];
 #pragma unroll
       for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          o[n] = mma<kOutPlanes, 1>(get_frag<F32, kOutPlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane), qf[ks], o[n]);
+          sum[n].template add<kOutPlanes, 1>(get_frag<F32, kOutPlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane), qf[ks]);
       pace<kAhead, kOutPieces, kMfma<F32, 2>, kKs * NT>();
       __builtin_amdgcn_sched_barrier(0);
       load_q(c + 1);
+      if (DELTA) lds_barrier();
       lds_barrier();
 #pragma unroll
-      for (int n = 0; n < NT; ++n) o[n] *= gq;
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < kOutParts; ++i) sum[n].s[i] *= gq;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          o[n] = mma<kOutPlanes, kOutPlanes>(get_frag<F32, kOutPlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane), to[ks], o[n]);
-      lds_barrier();
+          sum[n].template add<kOutPlanes, kOutPlanes>(get_frag<F32, kOutPlanes>(lds_o + (size_t)(ks * NT + n) * L::kOutFrag, lane), to[ks]);
+      f32x4 o[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[n] = sum[n].total();
       load_matrix(c + 1);
       if (token < len - c * kChunk) {
         if constexpr (NT == 1) {

@@ -40,24 +40,41 @@ struct Frag<true, N> {
 template <bool F32, int N>
 constexpr int kPiecesOf = F32 ? 2 : N;
 
-// c + a b of the first NA and NB planes, products of 2^-8 max(NA, NB) and less
-// of the whole left out, small ones first.
-template <int NA, int NB, int N, int M>
-__device__ __forceinline__ f32x4 mma(const Frag<false, N> &a, const Frag<false, M> &b, f32x4 c) {
-  constexpr int kMost = (NA > NB ? NA : NB) - 1;
+// A sum of products a b of the first NA and NB planes, those of 2^-8 max(NA, NB)
+// and less of the whole left out.  It is held in S parts, by the products' size: a
+// matrix instruction waits for the one before it on the same registers.
+template <int S>
+struct Sum {
+  f32x4 s[S];
+  __device__ __forceinline__ Sum() {
 #pragma unroll
-  for (int s = kMost; s >= 0; --s)
+    for (int i = 0; i < S; ++i) s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  template <int NA, int NB, int N, int M>
+  __device__ __forceinline__ void add(const Frag<false, N> &a, const Frag<false, M> &b) {
+    constexpr int kMost = (NA > NB ? NA : NB) - 1;
 #pragma unroll
     for (int i = 0; i < NA; ++i)
-      if (s - i >= 0 && s - i < NB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], c, 0, 0, 0);
-  return c;
-}
-template <int NA, int NB, int N, int M>
-__device__ __forceinline__ f32x4 mma(const Frag<true, N> &a, const Frag<true, M> &b, f32x4 c) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.p[e / 4][e % 4], b.p[e / 4][e % 4], c, 0, 0, 0);
-  return c;
-}
+      for (int j = 0; j < NB; ++j)
+        if (i + j <= kMost) {
+          f32x4 &c = s[i + j < S ? i + j : S - 1];
+          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], c, 0, 0, 0);
+        }
+  }
+  template <int NA, int NB, int N, int M>
+  __device__ __forceinline__ void add(const Frag<true, N> &a, const Frag<true, M> &b) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      s[e % S] = __builtin_amdgcn_mfma_f32_16x16x4f32(a.p[e / 4][e % 4], b.p[e / 4][e % 4], s[e % S], 0, 0, 0);
+  }
+  __device__ __forceinline__ f32x4 total() const {
+    f32x4 t = s[S - 1];
+#pragma unroll
+    for (int i = S - 2; i >= 0; --i) t += s[i];
+    return t;
+  }
+};
 
 // The bf16 planes of 4 values: the leading 8 bits of each, the next 8, the last
 // 8 (cut, not rounded: three planes are the value itself, and a mask and a
@@ -76,8 +93,8 @@ __device__ __forceinline__ void split4(const float (&x)[4], uint2 (&p)[N]) {
   }
 }
 
-// Planes of the two correction matrices: the one that makes the state, and the
-// one that makes outputs, which are rounded to bf16.
+// Planes of what the state depends on, and of what outputs alone do, which are
+// rounded to bf16.
 constexpr int kStatePlanes = 3, kOutPlanes = 2;
 
 // Row tile t of the lower triangular 64 x 64 matrices has the inner 32s ks <= t / 2.
@@ -85,7 +102,8 @@ __host__ __device__ constexpr int first_frag(int t) { return t < 2 ? t : 2 * t -
 constexpr int kTriFrags = 6;
 
 // What the first kernel leaves, operand by operand, 16 bytes a lane:
-//   for every (slot, head): to_state, to_out [6][pieces][64 lanes], decay [64] fp32;
+//   for every (slot, head): X beta and the decayed Q K^T, [6][pieces][64 lanes], and
+//   the decays G and D_63, fp32 [2][64];
 //   for every (slot, key head): K^T [d_k / 16][2][pieces][64 lanes], and K and Q
 //   [4][d_k / 32][pieces][64 lanes].  Keys and queries lie one token a row, often a
 //   power of two apart, so that a head's rows all fall to one channel of the L2; the
@@ -94,9 +112,10 @@ constexpr int kTriFrags = 6;
 template <bool F32, int DK>
 struct ChunkSpace {
   static constexpr size_t kPiece = 64 * 16;
-  static constexpr size_t kToState = kTriFrags * kPiecesOf<F32, kStatePlanes> * kPiece;
-  static constexpr size_t kToOut = kTriFrags * kPiecesOf<F32, kOutPlanes> * kPiece;
-  static constexpr size_t kHead = kToState + kToOut + kChunk * 4;
+  static constexpr size_t kSolve = kTriFrags * kPiecesOf<F32, kStatePlanes> * kPiece;
+  static constexpr size_t kMix = kTriFrags * kPiecesOf<F32, kOutPlanes> * kPiece;
+  static constexpr size_t kDecay = kSolve + kMix, kRest = kDecay + kChunk * 4;
+  static constexpr size_t kHead = kRest + kChunk * 4;
   static constexpr size_t kRows = 4 * (DK / 32) * kPiecesOf<F32, 1> * kPiece;  // of K, of Q, and of K^T
   static constexpr size_t kKeys = 3 * kRows;
 
