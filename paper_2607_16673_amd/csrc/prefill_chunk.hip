@@ -37,8 +37,10 @@ template <bool F32, int DK>
 struct MatricesLds {
   using T = typename std::conditional<F32, float, bf16>::type;
   static constexpr int kKeyPitch = DK + 16 / (int)sizeof(T);
-  T k[kChunk * kKeyPitch];
-  float x[kChunk * kPitch];  // L, then X
+  union {
+    T k[kChunk * kKeyPitch];
+    float x[kChunk * kPitch];  // L, then X, when the keys have been used: six workgroups to a CU instead of three
+  };
   float d[4][16][16];        // D inside the diagonal blocks
   float upto[kChunk];        // product of a block's gates up to i
   float behind[kChunk];      // product of a block's gates behind j
@@ -199,14 +201,48 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
     reinterpret_cast<float *>(head + space.kRest)[threadIdx.x] = s.rest[threadIdx.x];
   }
 
+  if (h % group == 0) {
+    unsigned char *keys = space.keys(slot, kh);
+#pragma unroll
+    for (int ks = 0; ks < DK / 32; ++ks)
+#pragma unroll
+      for (int j = 0; j < kPiecesOf<F32, 1>; ++j) {
+        const size_t at = (((size_t)wave * (DK / 32) + ks) * kPiecesOf<F32, 1> + j) * space.kPiece + lane * 16;
+        *reinterpret_cast<u32x4 *>(keys + space.kRows + at) =
+            reinterpret_cast<const u32x4 *>(s.k + tile_row(wave, r) * L::kKeyPitch + 32 * ks + 8 * g)[j];
+        *reinterpret_cast<u32x4 *>(keys + 2 * space.kRows + at) = reinterpret_cast<const u32x4 *>(&q[ks])[j];
+      }
+    for (int f = wave; f < DK / 16 * 2; f += kThreads / kWave) {
+      const T *from = s.k + (32 * (f % 2) + 8 * g) * L::kKeyPitch + tile_row(f / 2, r);
+      unsigned char *to = keys + (size_t)f * kPiecesOf<F32, 1> * space.kPiece;
+      if constexpr (F32) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = from[e * L::kKeyPitch];
+        store_frag<true, 1>(to, lane, x);
+      } else {
+        uint32_t x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = from[e * L::kKeyPitch].bits;
+        *reinterpret_cast<uint4 *>(to + lane * 16) =
+            make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
+      }
+    }
+  }
+
   if constexpr (DELTA) {
     // L: the row tile 3 - wave, which evens out the waves' products
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     const int rt = 3 - wave;
     Frag<F32, 1> kr[DK / 32];
 #pragma unroll
     for (int ks = 0; ks < DK / 32; ++ks) kr[ks] = key_frag(16 * rt + r, ks);
+    f32x4 low[4];
     float mid = 1.f;  // product of the blocks between the columns' and the rows'
-    for (int t = rt; t >= 0; --t) {
+#pragma unroll
+    for (int t = 3; t >= 0; --t) {
+      low[t] = zero;
+      if (t > rt) continue;
       Sum<1> sum;
 #pragma unroll
       for (int ks = 0; ks < DK / 32; ++ks) sum.template add<1, 1>(kr[ks], key_frag(16 * t + r, ks));
@@ -216,16 +252,15 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
       for (int i = 0; i < 4; ++i) {
         const int row = 16 * rt + 4 * g + i;
         const float d = t == rt ? s.d[rt][4 * g + i][r] : s.upto[row] * behind;
-        s.x[row * kPitch + 16 * t + r] = t == rt && 4 * g + i <= r ? 0.f : s.beta[row] * d * kk[i];
+        low[t][i] = t == rt && 4 * g + i <= r ? 0.f : s.beta[row] * d * kk[i];
       }
       if (t < rt) mid *= s.total[t];
     }
-    if (rt % 2 == 0)  // right of the diagonal: the operands reach there
-      block_store(s.x, rt, rt + 1, g, r, f32x4{0.f, 0.f, 0.f, 0.f});
-  }
-
-  if constexpr (DELTA) {
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    lds_barrier();  // every wave is done with the keys
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (t <= rt || (rt % 2 == 0 && t == rt + 1))  // the operands reach right of the diagonal
+        block_store(s.x, rt, t, g, r, low[t]);
     lds_barrier();
     {  // diagonal blocks: column r by forward substitution, in every 16 lanes alike
       float x[16];
@@ -273,34 +308,6 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = s.x[tile_row(wave, r) * kPitch + at + e] * s.beta[at + e];
       store_frag<F32, kStatePlanes>(head + (size_t)(first_frag(wave) + ks) * kPiecesOf<F32, kStatePlanes> * space.kPiece, lane, x);
-    }
-  }
-  if (h % group == 0) {
-    unsigned char *keys = space.keys(slot, kh);
-#pragma unroll
-    for (int ks = 0; ks < DK / 32; ++ks)
-#pragma unroll
-      for (int j = 0; j < kPiecesOf<F32, 1>; ++j) {
-        const size_t at = (((size_t)wave * (DK / 32) + ks) * kPiecesOf<F32, 1> + j) * space.kPiece + lane * 16;
-        *reinterpret_cast<u32x4 *>(keys + space.kRows + at) =
-            reinterpret_cast<const u32x4 *>(s.k + tile_row(wave, r) * L::kKeyPitch + 32 * ks + 8 * g)[j];
-        *reinterpret_cast<u32x4 *>(keys + 2 * space.kRows + at) = reinterpret_cast<const u32x4 *>(&q[ks])[j];
-      }
-    for (int f = wave; f < DK / 16 * 2; f += kThreads / kWave) {
-      const T *from = s.k + (32 * (f % 2) + 8 * g) * L::kKeyPitch + tile_row(f / 2, r);
-      unsigned char *to = keys + (size_t)f * kPiecesOf<F32, 1> * space.kPiece;
-      if constexpr (F32) {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = from[e * L::kKeyPitch];
-        store_frag<true, 1>(to, lane, x);
-      } else {
-        uint32_t x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = from[e * L::kKeyPitch].bits;
-        *reinterpret_cast<uint4 *>(to + lane * 16) =
-            make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
-      }
     }
   }
 }
@@ -354,17 +361,17 @@ __device__ __forceinline__ P load_piece(rsrc_t r, uint32_t voff, uint32_t soff) 
   return __builtin_bit_cast(P, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, kPolicyDefault));
 }
 
-// Reads of operands from LDS run `AHEAD` operands in front of the `FRAGS` ones'
-// products: R reads and M matrix instructions each.
-template <int AHEAD, int R, int M, int FRAGS>
+// The order of a phase: reads of operands from LDS run `AHEAD` operands in front of
+// the `FRAGS` ones' products, R reads and M matrix instructions each, and LOADS loads
+// from memory go in between, evenly: issued in a row, they would hold up the wave.
+template <int AHEAD, int R, int M, int FRAGS, int LOADS = 0, int F = 0>
 __device__ __forceinline__ void pace() {
-  constexpr int kFirst = AHEAD < FRAGS ? AHEAD : FRAGS;
-  __builtin_amdgcn_sched_group_barrier(0x100, R * kFirst, 0);
-#pragma unroll
-  for (int f = 0; f < FRAGS; ++f) {
-    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
-    if (f + kFirst < FRAGS) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
-  }
+  constexpr int kFirst = AHEAD < FRAGS ? AHEAD : FRAGS, kLoads = LOADS * (F + 1) / FRAGS - LOADS * F / FRAGS;
+  if constexpr (F == 0) __builtin_amdgcn_sched_group_barrier(0x100, R * kFirst, 0);
+  if constexpr (kLoads > 0) __builtin_amdgcn_sched_group_barrier(0x020, kLoads, 0);
+  __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+  if constexpr (F + kFirst < FRAGS) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  if constexpr (F + 1 < FRAGS) pace<AHEAD, R, M, FRAGS, LOADS, F + 1>();
 }
 
 // matrix instructions of one product of N planes
@@ -400,6 +407,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
   constexpr int kKs = DK / 32, kTiles = DK / 64, w = sizeof(T);
   constexpr int kKeyPieces = kPiecesOf<F32, 1>, kStatePieces = kPiecesOf<F32, kStatePlanes>, kOutPieces = kPiecesOf<F32, kOutPlanes>;
   constexpr int kParts = NT == 1 ? (F32 ? 2 : 3) : 1, kOutParts = NT == 1 ? 2 : 1;
+  constexpr bool kTwoSets = NT == 1 && DK <= (F32 ? 64 : 128);
   constexpr int kAhead = NT == 1 ? 8 : 2;  // of the state's operands read in front of their products
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   unsigned char *const lds_h = lds, *const lds_r = lds + L::kStateFrags * L::kFrag, *const lds_u = lds_r + L::kRowFrags * L::kFrag,
@@ -452,51 +460,52 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
 #pragma unroll
     for (int n = 0; n < NT; ++n)
       v_off[n] = col[n] < a.dv ? (uint32_t)(tile_row(wave, 4 * g) * (int)a.v_stride + col[n]) * w : kNowhere;
-    Frag<F32, 1> kf[kKs], key[kTiles][2];
-    Frag<F32, kStatePlanes> ts[2];
-    uint32_t vr[NT][4];
-    f32x4 gr, gu;  // decays of the rows 4 g + i, and behind them
-    float gc;  // of the whole chunk
-    auto load_k = [&](rsrc_t rs) {
+    struct Operands {
+      Frag<F32, 1> kf[kKs], key[kTiles][2];
+      Frag<F32, kStatePlanes> ts[2];
+      uint32_t vr[NT][4];
+      f32x4 gr, gu;  // decays of the rows 4 g + i, and behind them
+      float gc;      // of the whole chunk
+    };
+    auto load_k = [&](Operands &x, rsrc_t rs) {
 #pragma unroll
       for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
         for (int j = 0; j < kKeyPieces; ++j)
-          kf[ks].p[j] = load_piece<Piece>(rs, lane * 16 + j * kPiece, kRows + (wave * kKs + ks) * kKeyPieces * kPiece);
+          x.kf[ks].p[j] = load_piece<Piece>(rs, lane * 16 + j * kPiece, kRows + (wave * kKs + ks) * kKeyPieces * kPiece);
     };
-    auto load_v = [&](int c) {
+    auto load_v = [&](Operands &x, int c) {
       const rsrc_t rs = v_rows.next(c);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t row = (uint32_t)(i * (int)a.v_stride * w);
-          vr[n][i] = F32 ? __builtin_amdgcn_raw_buffer_load_b32(rs, v_off[n], row, kPolicyDefault)
+          x.vr[n][i] = F32 ? __builtin_amdgcn_raw_buffer_load_b32(rs, v_off[n], row, kPolicyDefault)
                          : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rs, v_off[n], row, kPolicyDefault);
         }
     };
-    auto load_decay = [&](rsrc_t rs) {
-      if (DELTA) gr = load_piece<f32x4>(rs, tile_row(wave, 4 * g) * 4, kDecay);
-      gu = load_piece<f32x4>(rs, tile_row(wave, 4 * g) * 4, kRest);
-      gc = buf_load_f32<kPolicyDefault>(rs, (kChunk - 1) * 4, kDecay);
+    auto load_decay = [&](Operands &x, rsrc_t rs) {
+      if (DELTA) x.gr = load_piece<f32x4>(rs, tile_row(wave, 4 * g) * 4, kDecay);
+      x.gu = load_piece<f32x4>(rs, tile_row(wave, 4 * g) * 4, kRest);
+      x.gc = buf_load_f32<kPolicyDefault>(rs, (kChunk - 1) * 4, kDecay);
     };
-    rsrc_t head = head_rows.next(0), keys = key_rows.next(0);
-    auto load_matrix = [&] {  // row tiles 0 and 1 have no second inner 32
+    auto load_matrix = [&](Operands &x, rsrc_t head) {  // row tiles 0 and 1 have no second inner 32
       const rsrc_t more = wave < 2 ? make_rsrc(head_rows.at, 0u) : head;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int j = 0; j < kStatePieces; ++j)
-          ts[ks].p[j] = load_piece<Piece>(ks ? more : head, lane * 16 + j * kPiece, (t0 + ks) * kStatePieces * kPiece);
+          x.ts[ks].p[j] = load_piece<Piece>(ks ? more : head, lane * 16 + j * kPiece, (t0 + ks) * kStatePieces * kPiece);
     };
-    auto load_keys = [&](rsrc_t rs) {
+    auto load_keys = [&](Operands &x, rsrc_t rs) {
 #pragma unroll
       for (int m = 0; m < kTiles; ++m)
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
           for (int j = 0; j < kKeyPieces; ++j)
-            key[m][ks].p[j] = load_piece<Piece>(rs, lane * 16 + j * kPiece, ((wave + 4 * m) * 2 + ks) * kKeyPieces * kPiece);
+            x.key[m][ks].p[j] = load_piece<Piece>(rs, lane * 16 + j * kPiece, ((wave + 4 * m) * 2 + ks) * kKeyPieces * kPiece);
     };
     auto put_state = [&](int m) {
 #pragma unroll
@@ -504,45 +513,43 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
         put_half<F32, kStatePlanes>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
     };
 
-    __builtin_amdgcn_s_setprio(2);
-    if (chunks > 0) {
-      if (DELTA) load_k(keys);
-      load_v(0);
-      load_decay(head);
-      if (DELTA) load_matrix();
-      load_keys(keys);
-    }
-#pragma unroll
-    for (int m = 0; m < kTiles; ++m) put_state(m);
-    for (int c = 0; c < chunks; ++c) {
+    // One chunk, from the operands `x`; the next one's go to `y`.  Where registers
+    // allow two sets, the loads lie between the products, a whole chunk ahead;
+    // else they follow the last use of their registers.
+    constexpr int kKeyLoads = 2 * kTiles * kKeyPieces, kRowLoads = kKs * kKeyPieces + 4 * NT, kSolveLoads = 2 * kStatePieces + 3;
+    auto step = [&](int c, Operands &x, Operands &y) {
       lds_barrier();
-      f32x4 hk[NT];
+      const rsrc_t head = head_rows.next(c + 1), keys = key_rows.next(c + 1);
+      f32x4 u[NT];  // V - G o (K H), then U
       if constexpr (DELTA) {
         Sum<kParts> sum[NT];
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            sum[n].template add<1, kStatePlanes>(kf[ks], get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane));
-        pace<kAhead, L::kPieces, kMfma<F32, 3>, kKs * NT>();
+            sum[n].template add<1, kStatePlanes>(x.kf[ks], get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane));
+        if (kTwoSets) {
+          load_k(y, keys);
+          load_v(y, c + 1);
+        }
+        pace<kAhead, L::kPieces, kMfma<F32, 3>, kKs * NT, kTwoSets ? kRowLoads : 0>();
         __builtin_amdgcn_sched_barrier(0);
+        if (!kTwoSets) load_k(y, keys);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) hk[n] = sum[n].total();
+        for (int n = 0; n < NT; ++n) u[n] = sum[n].total();
+      } else if (kTwoSets) {
+        load_v(y, c + 1);
       }
-      head = head_rows.next(c + 1);
-      keys = key_rows.next(c + 1);
-      if (DELTA) load_k(keys);
-      f32x4 u[NT];  // V - G o (K H), then U
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float v = __uint_as_float(F32 ? vr[n][i] : vr[n][i] << 16);
-          u[n][i] = DELTA ? __builtin_fmaf(-gr[i], hk[n][i], v) : v;
+          const float v = __uint_as_float(F32 ? x.vr[n][i] : x.vr[n][i] << 16);
+          u[n][i] = DELTA ? __builtin_fmaf(-x.gr[i], u[n][i], v) : v;
         }
         if (DELTA) put_half<F32, kStatePlanes>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, u[n]);
       }
-      load_v(c + 1);
+      if (!kTwoSets) load_v(y, c + 1);
       if constexpr (DELTA) {
         lds_barrier();
         Sum<kParts> sum[NT];
@@ -550,45 +557,74 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            sum[n].template add<kStatePlanes, kStatePlanes>(ts[ks], get_frag<F32, kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane));
-        pace<2, L::kPieces, F32 ? 8 : 6, 2 * NT>();
+            sum[n].template add<kStatePlanes, kStatePlanes>(x.ts[ks], get_frag<F32, kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane));
+        if (kTwoSets) {
+          load_matrix(y, head);
+          load_decay(y, head);
+        }
+        pace<2, L::kPieces, F32 ? 8 : 6, 2 * NT, kTwoSets ? kSolveLoads : 0>();
         __builtin_amdgcn_sched_barrier(0);
+        if (!kTwoSets) load_matrix(y, head);
 #pragma unroll
         for (int n = 0; n < NT; ++n) u[n] = sum[n].total();
-        load_matrix();
+      } else if (kTwoSets) {
+        load_decay(y, head);
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        put_half<F32, kStatePlanes>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, gu * u[n]);
+        put_half<F32, kStatePlanes>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, x.gu * u[n]);
         put_half<F32, kOutPlanes>(lds_o + (size_t)(wave / 2 * NT + n) * L::kOutFrag, half, lane, u[n]);
       }
-      const float whole = gc;
-      load_decay(head);
+      const float whole = x.gc;
+      if (!kTwoSets) load_decay(y, head);
       lds_barrier();
-      {
-        Sum<kParts> next[kTiles][NT];
+      Sum<kParts> next[kTiles][NT];
 #pragma unroll
-        for (int m = 0; m < kTiles; ++m)
+      for (int m = 0; m < kTiles; ++m)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) next[m][n].s[0] = H[m][n] * whole;
+        for (int n = 0; n < NT; ++n) next[m][n].s[0] = H[m][n] * whole;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+      for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const Frag<F32, kStatePlanes> uf = get_frag<F32, kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
+        for (int n = 0; n < NT; ++n) {
+          const Frag<F32, kStatePlanes> uf = get_frag<F32, kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
 #pragma unroll
-            for (int m = 0; m < kTiles; ++m) next[m][n].template add<1, kStatePlanes>(key[m][ks], uf);
-          }
-        pace<2, L::kPieces, kTiles * kMfma<F32, 3>, 2 * NT>();
-        __builtin_amdgcn_sched_barrier(0);
+          for (int m = 0; m < kTiles; ++m) next[m][n].template add<1, kStatePlanes>(x.key[m][ks], uf);
+        }
+      if (kTwoSets) load_keys(y, keys);
+      pace<2, L::kPieces, kTiles * kMfma<F32, 3>, 2 * NT, kTwoSets ? kKeyLoads : 0>();
+      __builtin_amdgcn_sched_barrier(0);
+      if (!kTwoSets) load_keys(y, keys);
 #pragma unroll
-        for (int m = 0; m < kTiles; ++m)
+      for (int m = 0; m < kTiles; ++m) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n) H[m][n] = next[m][n].total();
+        for (int n = 0; n < NT; ++n) H[m][n] = next[m][n].total();
+        put_state(m);
       }
-      load_keys(keys);
+    };
+
+    __builtin_amdgcn_s_setprio(2);
+    Operands even;
+    {
+      const rsrc_t head = head_rows.next(0), keys = key_rows.next(0);
+      if (chunks > 0) {
+        if (DELTA) load_k(even, keys);
+        load_v(even, 0);
+        if (DELTA) load_matrix(even, head);
+        load_decay(even, head);
+        load_keys(even, keys);
+      }
+    }
 #pragma unroll
-      for (int m = 0; m < kTiles; ++m) put_state(m);
+    for (int m = 0; m < kTiles; ++m) put_state(m);
+    if constexpr (kTwoSets) {
+      Operands odd;
+      for (int c = 0; c < chunks; c += 2) {
+        step(c, even, odd);
+        if (c + 1 < chunks) step(c + 1, odd, even);
+      }
+    } else {
+      for (int c = 0; c < chunks; ++c) step(c, even, even);
     }
 #pragma unroll
     for (int m = 0; m < kTiles; ++m)
