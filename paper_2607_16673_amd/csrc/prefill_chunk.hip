@@ -107,14 +107,18 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
   if (c.b < 0 || c.rows == 0) return;
 
   // keys to LDS, queries to registers, gates
-  constexpr int kLanes = DK / 8;
+  const size_t gate = (size_t)(c.row + min(lane, c.rows - 1)) * a.H + h;
+  const float alpha = a.alpha ? a.alpha[gate] : 1.f, beta = DELTA ? a.beta[gate] : 1.f;
+  // (rows past the end repeat the last one until they are zeroed, so that no load waits for a branch)
+  constexpr int kLanes = DK / 8, kLoads = kChunk * kLanes / kThreads, kWords = sizeof(T) / 2;
   const T *k = static_cast<const T *>(a.k) + (int64_t)c.row * a.k_stride + (size_t)kh * DK;
-  for (int i = threadIdx.x; i < kChunk * kLanes; i += kThreads) {
-    const int t = i / kLanes, e = i % kLanes * 8;
-    u32x4 *to = reinterpret_cast<u32x4 *>(s.k + t * L::kKeyPitch + e);
-    const u32x4 *from = reinterpret_cast<const u32x4 *>(k + (int64_t)t * a.k_stride + e);
+  u32x4 staged[kLoads][kWords];
 #pragma unroll
-    for (int j = 0; j < (int)sizeof(T) / 2; ++j) to[j] = t < c.rows ? from[j] : u32x4{0, 0, 0, 0};
+  for (int i = 0; i < kLoads; ++i) {
+    const int t = (threadIdx.x + i * kThreads) / kLanes, e = threadIdx.x % kLanes * 8;
+#pragma unroll
+    for (int j = 0; j < kWords; ++j)
+      staged[i][j] = reinterpret_cast<const u32x4 *>(k + (int64_t)min(t, c.rows - 1) * a.k_stride + e)[j];
   }
   Frag<F32, 1> q[DK / 32];
   {
@@ -129,11 +133,17 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
         reinterpret_cast<u32x4 *>(&q[ks])[j] = x;
       }
   }
-  const size_t gate = (size_t)c.row * a.H + h;
-  if (wave == 1) s.beta[lane] = lane < c.rows ? (DELTA ? a.beta[gate + (size_t)lane * a.H] : 1.f) : 0.f;
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int t = (threadIdx.x + i * kThreads) / kLanes, e = threadIdx.x % kLanes * 8;
+#pragma unroll
+    for (int j = 0; j < kWords; ++j)
+      reinterpret_cast<u32x4 *>(s.k + t * L::kKeyPitch + e)[j] = t < c.rows ? staged[i][j] : u32x4{0, 0, 0, 0};
+  }
+  if (wave == 1) s.beta[lane] = lane < c.rows ? beta : 0.f;
   if (wave == 0) {
     // lane 16 b + j: column j of D's diagonal block b, and the products along the block
-    const float al = a.alpha && lane < c.rows ? a.alpha[gate + (size_t)lane * a.H] : 1.f;
+    const float al = lane < c.rows ? alpha : 1.f;
     float col = 0.f, run = 1.f, upto = 1.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {

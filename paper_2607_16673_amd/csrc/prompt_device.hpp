@@ -59,9 +59,9 @@ __device__ __forceinline__ Chunk find_chunk(const PackedRows &r, int slot, int l
   const int b = before - 1, start = r.start[b], end = r.start[b + 1];
   const int at = slot - (start / C + b);
   if (at > 0 && (int64_t)at * C >= end - start) return c;
-  c.b = b;
-  c.row = start + at * C;
-  c.rows = min(C, end - c.row);
+  c.b = __builtin_amdgcn_readfirstlane(b);
+  c.row = __builtin_amdgcn_readfirstlane(start + at * C);
+  c.rows = __builtin_amdgcn_readfirstlane(min(C, end - c.row));
   c.first = at == 0;
   c.last = c.row + c.rows == end;
   return c;
