@@ -41,10 +41,10 @@ __global__ __launch_bounds__(kThreads) void serial_kernel(PrefillArgs a, int sla
   const int slab = (int)(wg % (unsigned)slabs);
   if (unit >= (unsigned)a.rows.B * (unsigned)a.H) return;
   const int b = (int)(unit / (unsigned)a.H), h = (int)(unit % (unsigned)a.H);
+  const int start = a.rows.start[b], len = a.rows.start[b + 1] - start;
   const bool ok = starts_ok(a.rows, lane);
   if (a.status && h == 0 && slab == 0 && threadIdx.x == 0) a.status[b] = ok ? SLA_OK : SLA_ERR_LENGTH;
   if (!ok) return;
-  const int start = a.rows.start[b], len = a.rows.start[b + 1] - start;
   const int col = slab * kCols + cl * 4;
   const bool live = col < a.dv;
   const int kh = h / (a.H / a.Hk);

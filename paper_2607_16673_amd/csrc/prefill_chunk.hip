@@ -133,13 +133,6 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
         reinterpret_cast<u32x4 *>(&q[ks])[j] = x;
       }
   }
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int t = (threadIdx.x + i * kThreads) / kLanes, e = threadIdx.x % kLanes * 8;
-#pragma unroll
-    for (int j = 0; j < kWords; ++j)
-      reinterpret_cast<u32x4 *>(s.k + t * L::kKeyPitch + e)[j] = t < c.rows ? staged[i][j] : u32x4{0, 0, 0, 0};
-  }
   if (wave == 1) s.beta[lane] = lane < c.rows ? beta : 0.f;
   if (wave == 0) {
     // lane 16 b + j: column j of D's diagonal block b, and the products along the block
@@ -162,6 +155,13 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
     s.decay[lane] = front * upto;
     s.rest[lane] = col * back;
   }
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int t = (threadIdx.x + i * kThreads) / kLanes, e = threadIdx.x % kLanes * 8;
+#pragma unroll
+    for (int j = 0; j < kWords; ++j)
+      reinterpret_cast<u32x4 *>(s.k + t * L::kKeyPitch + e)[j] = t < c.rows ? staged[i][j] : u32x4{0, 0, 0, 0};
+  }
   lds_barrier();
 
   unsigned char *const head = space.head(slot, h);
@@ -177,14 +177,13 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
   {
     const int query = 16 * wave + r;
     const float upto = s.upto[query];
+    float p[2][8];  // row tiles 0 and 1 have no second inner 32; it is made all the same, without a branch
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
-      if (ks > wave / 2) continue;
       const int block = 2 * ks + g / 2;  // of the lane's keys
       float mid = upto;                  // ... times the blocks between
-      if (wave - block > 1) mid *= s.total[block + 1];
-      if (wave - block > 2) mid *= s.total[block + 2];
-      float p[8];
+      mid *= wave - block > 1 ? s.total[block + 1 & 3] : 1.f;
+      mid *= wave - block > 2 ? s.total[block + 2 & 3] : 1.f;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         Sum<2> sum;
@@ -201,10 +200,13 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
         const f32x4 behind = *reinterpret_cast<const f32x4 *>(s.behind + key);
         const f32x4 same = *reinterpret_cast<const f32x4 *>(&s.d[wave][r][key % 16]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[4 * t + i] = key + i > query ? 0.f : qk[i] * (block == wave ? same[i] : mid * behind[i]);
+        for (int i = 0; i < 4; ++i) p[ks][4 * t + i] = key + i > query ? 0.f : qk[i] * (block == wave ? same[i] : mid * behind[i]);
       }
-      store_frag<F32, kOutPlanes>(head + space.kSolve + (size_t)(first_frag(wave) + ks) * kPiecesOf<F32, kOutPlanes> * space.kPiece, lane, p);
     }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+      if (ks <= wave / 2)
+        store_frag<F32, kOutPlanes>(head + space.kSolve + (size_t)(first_frag(wave) + ks) * kPiecesOf<F32, kOutPlanes> * space.kPiece, lane, p[ks]);
   }
   if (threadIdx.x < kChunk) {
     reinterpret_cast<float *>(head + space.kDecay)[threadIdx.x] = s.decay[threadIdx.x];
@@ -241,49 +243,50 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
   }
 
   if constexpr (DELTA) {
-    // L: the row tile 3 - wave, which evens out the waves' products
+    // L: the 12 tiles up to the ones right of the diagonal, which the operands reach
+    // (those are zeros); three to a wave
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    const int rt = 3 - wave;
-    Frag<F32, 1> kr[DK / 32];
+    f32x4 low[3];
+    int ti[3], tj[3];
 #pragma unroll
-    for (int ks = 0; ks < DK / 32; ++ks) kr[ks] = key_frag(16 * rt + r, ks);
-    f32x4 low[4];
-    float mid = 1.f;  // product of the blocks between the columns' and the rows'
-#pragma unroll
-    for (int t = 3; t >= 0; --t) {
-      low[t] = zero;
-      if (t > rt) continue;
+    for (int n = 0; n < 3; ++n) {
+      const int tile = 3 * wave + n;  // (0, 0) (0, 1) (1, 0) (1, 1) (2, 0) .. (2, 3) (3, 0) .. (3, 3)
+      ti[n] = tile < 4 ? tile / 2 : tile / 4 + 1;
+      tj[n] = tile < 4 ? tile % 2 : tile % 4;
       Sum<1> sum;
 #pragma unroll
-      for (int ks = 0; ks < DK / 32; ++ks) sum.template add<1, 1>(kr[ks], key_frag(16 * t + r, ks));
+      for (int ks = 0; ks < DK / 32; ++ks) sum.template add<1, 1>(key_frag(16 * ti[n] + r, ks), key_frag(16 * tj[n] + r, ks));
       const f32x4 kk = sum.total();
-      const float behind = s.behind[16 * t + r] * mid;
+      float behind = s.behind[16 * tj[n] + r];
+      behind *= ti[n] - tj[n] > 1 ? s.total[tj[n] + 1 & 3] : 1.f;
+      behind *= ti[n] - tj[n] > 2 ? s.total[tj[n] + 2 & 3] : 1.f;
+      const int row = 16 * ti[n] + 4 * g, col = 16 * tj[n] + r;
+      const f32x4 beta = *reinterpret_cast<const f32x4 *>(s.beta + row), upto = *reinterpret_cast<const f32x4 *>(s.upto + row);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int row = 16 * rt + 4 * g + i;
-        const float d = t == rt ? s.d[rt][4 * g + i][r] : s.upto[row] * behind;
-        low[t][i] = t == rt && 4 * g + i <= r ? 0.f : s.beta[row] * d * kk[i];
+        const float d = ti[n] == tj[n] ? s.d[ti[n]][4 * g + i][r] : upto[i] * behind;
+        low[n][i] = row + i <= col ? 0.f : beta[i] * d * kk[i];
       }
-      if (t < rt) mid *= s.total[t];
     }
     lds_barrier();  // every wave is done with the keys
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-      if (t <= rt || (rt % 2 == 0 && t == rt + 1))  // the operands reach right of the diagonal
-        block_store(s.x, rt, t, g, r, low[t]);
+    for (int n = 0; n < 3; ++n) block_store(s.x, ti[n], tj[n], g, r, low[n]);
     lds_barrier();
     {  // diagonal blocks: column r by forward substitution, in every 16 lanes alike
       float x[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        x[i] = i == r ? 1.f : 0.f;
+      for (int i = 0; i < 16; ++i) x[i] = i == r ? 1.f : 0.f;
 #pragma unroll
-        for (int j4 = 0; j4 < (i + 3) / 4; ++j4) {
-          const f32x4 l = *reinterpret_cast<const f32x4 *>(s.x + (16 * wave + i) * kPitch + 16 * wave + 4 * j4);
+      for (int p = 0; p < 4; ++p) {  // four columns of L: what is known of x goes to all rows below at once
+        f32x4 l[16];
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (4 * j4 + j < i) x[i] = __builtin_fmaf(-l[j], x[4 * j4 + j], x[i]);
-        }
+        for (int i = 4 * p + 1; i < 16; ++i)
+          l[i] = *reinterpret_cast<const f32x4 *>(s.x + (16 * wave + i) * kPitch + 16 * wave + 4 * p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 4 * p + 1; i < 16; ++i)
+            if (i > 4 * p + j) x[i] = __builtin_fmaf(-l[i][j], x[4 * p + j], x[i]);
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i)
@@ -433,11 +436,11 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
   const int slab = (int)(at % (unsigned)slabs);
   if (unit >= (unsigned)a.rows.B * (unsigned)a.H) return;
   const int b = (int)(unit / (unsigned)a.H), h = (int)(unit % (unsigned)a.H), kh = h / (a.H / a.Hk);
+  const int start = __builtin_amdgcn_readfirstlane(a.rows.start[b]);
+  const int len = __builtin_amdgcn_readfirstlane(a.rows.start[b + 1]) - start;
   const bool ok = starts_ok(a.rows, lane);
   if (a.status && h == 0 && slab == 0 && threadIdx.x == 0) a.status[b] = ok ? SLA_OK : SLA_ERR_LENGTH;
   if (!ok) return;
-  const int start = __builtin_amdgcn_readfirstlane(a.rows.start[b]);
-  const int len = __builtin_amdgcn_readfirstlane(a.rows.start[b + 1]) - start;
   const int chunks = (len + kChunk - 1) / kChunk, last = chunks - 1, tail = len - last * kChunk;
   const size_t slot0 = (size_t)(start / kChunk) + b;
   auto rows_of = [&](const void *p, int64_t stride, size_t first, int width) {

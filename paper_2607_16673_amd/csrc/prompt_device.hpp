@@ -46,17 +46,20 @@ struct Chunk {
 template <int C>
 __device__ __forceinline__ Chunk find_chunk(const PackedRows &r, int slot, int lane, bool &ok) {
   bool bad = false;
-  int before = 0;
+  int before = 0, a = 0, e = 0;
   for (int i = lane; i - lane < r.B; i += kWave) {
     const bool live = i < r.B;
-    const int a = live ? r.start[i] : 0, b = live ? r.start[i + 1] : 0;
-    bad = bad || (live && (a < 0 || a > b || b > r.tokens));
+    a = live ? r.start[i] : 0;
+    e = live ? r.start[i + 1] : 0;
+    bad = bad || (live && (a < 0 || a > e || e > r.tokens));
     before += __popcll(__ballot(live && a / C + i <= slot));
   }
   ok = !wave_any(bad);
   Chunk c = {-1, 0, 0, false, false};
   if (!ok || before == 0) return c;
-  const int b = before - 1, start = r.start[b], end = r.start[b + 1];
+  // (the last 64 sequences' starts are at hand)
+  const int b = before - 1, kept = b - (r.B - 1) / kWave * kWave;
+  const int start = kept >= 0 ? __shfl(a, kept) : r.start[b], end = kept >= 0 ? __shfl(e, kept) : r.start[b + 1];
   const int at = slot - (start / C + b);
   if (at > 0 && (int64_t)at * C >= end - start) return c;
   c.b = __builtin_amdgcn_readfirstlane(b);
