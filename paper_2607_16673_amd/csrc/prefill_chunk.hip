@@ -432,10 +432,11 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
 
   // the slabs of a head, and neighbouring heads, one behind another on one XCD
   const unsigned wg = workgroup(), at = wg / kXcdCount;
-  const unsigned unit = at / (unsigned)slabs * kXcdCount + wg % kXcdCount;
+  const unsigned place = at / (unsigned)slabs * kXcdCount + wg % kXcdCount;
   const int slab = (int)(at % (unsigned)slabs);
-  if (unit >= (unsigned)a.rows.B * (unsigned)a.H) return;
-  const int b = (int)(unit / (unsigned)a.H), h = (int)(unit % (unsigned)a.H), kh = h / (a.H / a.Hk);
+  if (place >= (unsigned)a.rows.B * (unsigned)a.H) return;
+  const int b = by_length(a.rows, (int)(place / (unsigned)a.H), lane), h = (int)(place % (unsigned)a.H), kh = h / (a.H / a.Hk);
+  const size_t unit = (size_t)b * a.H + h;
   const int start = __builtin_amdgcn_readfirstlane(a.rows.start[b]);
   const int len = __builtin_amdgcn_readfirstlane(a.rows.start[b + 1]) - start;
   const bool ok = starts_ok(a.rows, lane);
@@ -466,7 +467,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           H[m][n][i] = a.state && col[n] < a.dv
-                           ? a.state[((size_t)unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] : 0.f;
+                           ? a.state[(unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] : 0.f;
 
     ChunkRows v_rows = rows_of(a.v, a.v_stride, (size_t)h * a.dv, a.dv);
     uint32_t v_off[NT];
@@ -645,7 +646,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (col[n] < a.dv) a.state_out[((size_t)unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] = H[m][n][i];
+          if (col[n] < a.dv) a.state_out[(unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] = H[m][n][i];
   } else {
     // lane: token 16 wave + r, columns 4 g + i of each tile
     const int token = 16 * wave + r;

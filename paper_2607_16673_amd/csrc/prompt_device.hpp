@@ -33,6 +33,20 @@ __host__ __device__ inline int64_t chunk_slots(const PackedRows &r) {
   return (int64_t)r.tokens / C + r.B;
 }
 
+// The sequence to be begun as number `place`: the longest first, for batches of up
+// to 64, so that no long one is begun when the others have ended; else in order.
+// (Wave-uniform; starts need not be in order.)
+__device__ __forceinline__ int by_length(const PackedRows &r, int place, int lane) {
+  if (r.B > kWave) return place;
+  const int len = lane < r.B ? r.start[lane + 1] - r.start[lane] : 0;
+  int rank = lane < r.B ? 0 : -1;
+  for (int i = 0; i < r.B; ++i) {
+    const int other = __builtin_amdgcn_readlane(len, i);
+    rank += lane < r.B && (other > len || (other == len && i < lane));
+  }
+  return __builtin_ctzll(__ballot(rank == place));
+}
+
 struct Chunk {
   int b;      // sequence, -1: none
   int row;    // first row
