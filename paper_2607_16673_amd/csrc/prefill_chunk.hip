@@ -420,6 +420,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
   constexpr int kKs = DK / 32, kTiles = DK / 64, w = sizeof(T);
   constexpr int kKeyPieces = kPiecesOf<F32, 1>, kStatePieces = kPiecesOf<F32, kStatePlanes>, kOutPieces = kPiecesOf<F32, kOutPlanes>;
   constexpr int kParts = NT == 1 ? (F32 ? 2 : 3) : 1, kOutParts = NT == 1 ? 2 : 1;
+  constexpr bool kTouch = kWavesPerSimd<F32, DK, NT> == 2;
   constexpr bool kTwoSets = NT == 1 && DK <= (F32 ? 64 : 128);
   constexpr int kAhead = NT == 1 ? 8 : 2;  // of the state's operands read in front of their products
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -451,6 +452,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
   };
   ChunkRows head_rows = {space.head(slot0, h), (int64_t)(a.H * space.kHead), (uint32_t)space.kHead, (uint32_t)space.kHead, last};
   ChunkRows key_rows = {space.keys(slot0, kh), (int64_t)(a.Hk * space.kKeys), (uint32_t)space.kKeys, (uint32_t)space.kKeys, last};
+  constexpr int kHeadLines = ChunkSpace<F32, DK>::kHead / 128, kLines = kHeadLines + ChunkSpace<F32, DK>::kKeys / 128;
   const int t0 = first_frag(wave);
   constexpr uint32_t kDecay = ChunkSpace<F32, DK>::kDecay, kRest = ChunkSpace<F32, DK>::kRest;
   constexpr uint32_t kPiece = ChunkSpace<F32, DK>::kPiece, kRows = ChunkSpace<F32, DK>::kRows;
@@ -488,8 +490,9 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
         for (int j = 0; j < kKeyPieces; ++j)
           x.kf[ks].p[j] = load_piece<Piece>(rs, lane * 16 + j * kPiece, kRows + (wave * kKs + ks) * kKeyPieces * kPiece);
     };
-    auto load_v = [&](Operands &x, int c) {
+    auto load_v = [&](Operands &x, int c, rsrc_t head) {
       const rsrc_t rs = v_rows.next(c);
+      if (DELTA) x.gr = load_piece<f32x4>(head, tile_row(wave, 4 * g) * 4, kDecay);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -500,7 +503,6 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
         }
     };
     auto load_decay = [&](Operands &x, rsrc_t rs) {
-      if (DELTA) x.gr = load_piece<f32x4>(rs, tile_row(wave, 4 * g) * 4, kDecay);
       x.gu = load_piece<f32x4>(rs, tile_row(wave, 4 * g) * 4, kRest);
       x.gc = buf_load_f32<kPolicyDefault>(rs, (kChunk - 1) * 4, kDecay);
     };
@@ -530,7 +532,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
     // One chunk, from the operands `x`; the next one's go to `y`.  Where registers
     // allow two sets, the loads lie between the products, a whole chunk ahead;
     // else they follow the last use of their registers.
-    constexpr int kKeyLoads = 2 * kTiles * kKeyPieces, kRowLoads = kKs * kKeyPieces + 4 * NT, kSolveLoads = 2 * kStatePieces + 3;
+    constexpr int kKeyLoads = 2 * kTiles * kKeyPieces, kRowLoads = kKs * kKeyPieces + 4 * NT + 1, kSolveLoads = 2 * kStatePieces + 2;
     auto step = [&](int c, Operands &x, Operands &y) {
       lds_barrier();
       const rsrc_t head = head_rows.next(c + 1), keys = key_rows.next(c + 1);
@@ -544,7 +546,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
             sum[n].template add<1, kStatePlanes>(x.kf[ks], get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane));
         if (kTwoSets) {
           load_k(y, keys);
-          load_v(y, c + 1);
+          load_v(y, c + 1, head);
         }
         pace<kAhead, L::kPieces, kMfma<F32, 3>, kKs * NT, kTwoSets ? kRowLoads : 0>();
         __builtin_amdgcn_sched_barrier(0);
@@ -552,7 +554,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
 #pragma unroll
         for (int n = 0; n < NT; ++n) u[n] = sum[n].total();
       } else if (kTwoSets) {
-        load_v(y, c + 1);
+        load_v(y, c + 1, head);
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -563,7 +565,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
         }
         if (DELTA) put_half<F32, kStatePlanes>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, u[n]);
       }
-      if (!kTwoSets) load_v(y, c + 1);
+      if (!kTwoSets) load_v(y, c + 1, head);
       if constexpr (DELTA) {
         lds_barrier();
         Sum<kParts> sum[NT];
@@ -623,7 +625,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       const rsrc_t head = head_rows.next(0), keys = key_rows.next(0);
       if (chunks > 0) {
         if (DELTA) load_k(even, keys);
-        load_v(even, 0);
+        load_v(even, 0, head);
         if (DELTA) load_matrix(even, head);
         load_decay(even, head);
         load_keys(even, keys);
@@ -633,10 +635,12 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
     for (int m = 0; m < kTiles; ++m) put_state(m);
     if constexpr (kTwoSets) {
       Operands odd;
-      for (int c = 0; c < chunks; c += 2) {
+      int c = 0;
+      for (; c + 1 < chunks; c += 2) {  // (with no branch between the two, which would wait for all loads)
         step(c, even, odd);
-        if (c + 1 < chunks) step(c + 1, odd, even);
+        step(c + 1, odd, even);
       }
+      if (c < chunks) step(c, even, odd);
     } else {
       for (int c = 0; c < chunks; ++c) step(c, even, even);
     }
@@ -673,9 +677,28 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
                                           ChunkSpace<F32, DK>::kSolve + (t0 + ks) * kOutPieces * kPiece);
       gq = buf_load_f32<kPolicyDefault>(rs, token * 4, kDecay);
     };
+    // Where one workgroup has a CU, nothing else runs while its loads take their time.
+    // The lines that the head's workgroups will read two chunks on are brought to the
+    // L2 by one load a wave, whose bytes nothing looks at: a part of the operands by
+    // each workgroup, and its own values.  (Every wave loads every time, past the end
+    // the last line again: a load that may not be there makes others wait for all.)
+    const int line = min((wave * kWave + lane) * slabs + slab, kLines - 1);
+    const bool of_head = line < kHeadLines;
+    const unsigned char *const lines = of_head ? space.head(slot0, h) + (size_t)line * 128
+                                               : space.keys(slot0, kh) + (size_t)(line - kHeadLines) * 128;
+    const size_t line_step = of_head ? a.H * space.kHead : a.Hk * space.kKeys;
+    const T *const values = static_cast<const T *>(a.v) + start * a.v_stride + (size_t)h * a.dv + min(slab * 16 * NT, a.dv - 16);
+    uint32_t seen[2] = {};
+    auto touch = [&](int c) {
+      if (!kTouch) return;
+      asm volatile("" ::"v"(seen[0]), "v"(seen[1]));  // the last ones' use: a chunk later they are there
+      seen[0] = *reinterpret_cast<const uint32_t *>(lines + min(c, last) * line_step);
+      seen[1] = *reinterpret_cast<const uint32_t *>(values + (int64_t)min(c * kChunk + 16 * wave + r, len - 1) * a.v_stride);
+    };
     if (chunks > 0) {
       load_q(0);
       load_matrix(0);
+      touch(1);
     }
     for (int c = 0; c < chunks; ++c) {
       lds_barrier();
@@ -703,6 +726,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
 #pragma unroll
       for (int n = 0; n < NT; ++n) o[n] = sum[n].total();
       load_matrix(c + 1);
+      touch(c + 2);
       if (token < len - c * kChunk) {
         if constexpr (NT == 1) {
           const float x[4] = {o[0][0], o[0][1], o[0][2], o[0][3]};
@@ -717,6 +741,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       }
       out += out_step;
     }
+    asm volatile("" ::"v"(seen[0]), "v"(seen[1]));
   }
 }
 
