@@ -554,8 +554,8 @@ int sla_page_copy(const sla_attn_shape *shape, int32_t layers, void *k_cache, vo
  * and z multiples of 16 bytes and of at most 2^22 elements, else
  * SLA_ERR_UNSUPPORTED.  With no rows (tokens = 0, rows = 0) the pointers to
  * rows may be NULL.  Results are the same from run to run, and a sequence's do
- * not depend on the others of its batch, but for sla_prefill's last bits, where
- * the rows are at most four times the sequences in one call and more in another. */
+ * not depend on the others of its batch, but for the last bits of sla_prefill of
+ * short sequences, which go by the call's rows and sequences. */
 
 typedef struct sla_prefill_shape {
   int32_t tokens;    /* rows T of q, k, v and out, 0..2^30                     */

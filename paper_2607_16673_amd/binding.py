@@ -500,8 +500,6 @@ def sla_recurrent_inputs(q, k, a, b, a_log, dt_bias, q_out, k_out, alpha, beta, 
     [H] fp32 (dt_bias may be None); q_out, k_out [N][r Hk][dk], every head r times;
     alpha, beta [N][H] fp32 (None with its input: not computed).  q_scale defaults
     to dk^-0.5."""
-    if q_scale is None:
-        q_scale = q.shape[-1] ** -0.5
     code = (_nat or native()).recurrent_inputs(q, k, a, b, a_log, dt_bias, q_out, k_out, alpha, beta, q_scale, eps)
     _check(code, "sla_recurrent_inputs")
 

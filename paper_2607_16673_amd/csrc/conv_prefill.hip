@@ -59,9 +59,9 @@ __global__ __launch_bounds__(kThreads) void conv_prefill_kernel(ConvPrefillArgs 
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const unsigned wg = workgroup();
   const int slot = (int)(wg / (unsigned)chunks), chunk = (int)(wg % (unsigned)chunks);
-  if (slot >= chunk_slots<kTokens>(a.rows)) return;
+  if (slot >= chunk_slots<kTokens>(a.rows, -1)) return;
   bool ok;
-  const Chunk c = find_chunk<kTokens>(a.rows, slot, lane, ok);
+  const Chunk c = find_chunk<kTokens>(a.rows, -1, slot, lane, ok);
   if (a.status && chunk == 0 && threadIdx.x == 0) {
     if (!ok && slot < a.rows.B) a.status[slot] = SLA_ERR_LENGTH;
     if (ok && c.b >= 0 && c.first) a.status[c.b] = SLA_OK;
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kThreads) void conv_prefill_kernel(ConvPrefillArgs 
 template <typename T, int K>
 hipError_t launch_k(const ConvPrefillArgs &a, hipStream_t s) {
   const int chunks = (a.D + kChannels - 1) / kChannels;
-  hipLaunchKernelGGL((conv_prefill_kernel<T, K>), grid_of((uint64_t)chunk_slots<kTokens>(a.rows) * chunks), dim3(kThreads), 0, s,
+  hipLaunchKernelGGL((conv_prefill_kernel<T, K>), grid_of((uint64_t)chunk_slots<kTokens>(a.rows, -1) * chunks), dim3(kThreads), 0, s,
                      a, chunks);
   return hipGetLastError();
 }

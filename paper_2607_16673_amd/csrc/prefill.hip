@@ -1,4 +1,5 @@
-// prefill.hip -- the recurrence over packed sequences, token by token.
+// prefill.hip -- the recurrence over packed sequences: which of them go token by
+// token and which in chunks (prefill_chunk.hip), and the kernel of the former.
 //
 // One workgroup = one (sequence, head) and 64 columns of its state, which stay in
 // registers from the first token to the last: wave w holds the rows w dk / 4 ..,
@@ -43,6 +44,7 @@ __global__ __launch_bounds__(kThreads) void serial_kernel(PrefillArgs a, int sla
   const int b = (int)(unit / (unsigned)a.H), h = (int)(unit % (unsigned)a.H);
   const int start = a.rows.start[b], len = a.rows.start[b + 1] - start;
   const bool ok = starts_ok(a.rows, lane);
+  if (ok && len > a.serial_len) return;
   if (a.status && h == 0 && slab == 0 && threadIdx.x == 0) a.status[b] = ok ? SLA_OK : SLA_ERR_LENGTH;
   if (!ok) return;
   const int col = slab * kCols + cl * 4;
@@ -137,14 +139,28 @@ hipError_t launch_serial(const PrefillArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Sequences of about a token take the serial kernel: it streams the states once,
-// in one launch, where the chunked ones need a chunk's matrices first.
-bool serial(const PrefillArgs &a) { return a.rows.tokens <= 4 * (int64_t)a.rows.B; }
+// Which sequences go token by token: a chunk takes the chunked kernels about as long
+// whether it is full or not.  16 heads of 128, microseconds token by token and in
+// chunks: one sequence of 6 tokens 11.8 and 13.7, of 8 tokens 14.7 and 13.7; 256
+// sequences, whose states fill the chip, of 4 tokens 126 and 452, of 24 tokens 388 and
+// 464.  Where all tokens together are no more, one launch does; where there are 64 a
+// sequence, all go in chunks, without the launch for short ones among them.
+PrefillArgs divided(PrefillArgs a) {
+  const int64_t workgroups = (int64_t)a.rows.B * a.H * ((a.dv + kCols - 1) / kCols);
+  a.serial_len = workgroups >= 4 * device_cus() ? 24 : 6;
+  if (a.rows.tokens >= 64 * (int64_t)a.rows.B) a.serial_len = -1;
+  return a;
+}
+bool all_serial(const PrefillArgs &a) { return a.rows.tokens <= a.serial_len; }
 
 template <bool F32, int DK>
 hipError_t launch_dk(const PrefillArgs &a, hipStream_t s) {
   using T = typename std::conditional<F32, float, bf16>::type;
-  return serial(a) ? launch_serial<T, DK>(a, s) : launch_chunks<F32, DK>(a, s);
+  if (a.serial_len >= 0) {
+    const hipError_t e = launch_serial<T, DK>(a, s);
+    if (e != hipSuccess || all_serial(a)) return e;
+  }
+  return launch_chunks<F32, DK>(a, s);
 }
 
 template <bool F32>
@@ -167,13 +183,14 @@ size_t bytes_t(const PrefillArgs &a) {
 
 }  // namespace
 
-size_t prefill_workspace_bytes(const PrefillArgs &a, int dtype) {
-  if (serial(a)) return 0;
+size_t prefill_workspace_bytes(const PrefillArgs &args, int dtype) {
+  const PrefillArgs a = divided(args);
+  if (all_serial(a)) return 0;
   return dtype == SLA_DTYPE_BF16 ? bytes_t<false>(a) : bytes_t<true>(a);
 }
 
 hipError_t launch_prefill(const PrefillArgs &a, int dtype, hipStream_t s) {
-  return dtype == SLA_DTYPE_BF16 ? launch_t<false>(a, s) : launch_t<true>(a, s);
+  return dtype == SLA_DTYPE_BF16 ? launch_t<false>(divided(a), s) : launch_t<true>(divided(a), s);
 }
 
 }  // namespace sla

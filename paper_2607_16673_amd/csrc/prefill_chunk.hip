@@ -103,7 +103,20 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
   const int h = (int)(wg % (unsigned)a.H), group = a.H / a.Hk, kh = h / group;
   if (slot >= space.slots) return;
   bool ok;
-  const Chunk c = find_chunk<kChunk>(a.rows, (int)slot, lane, ok);
+  const Chunk c = find_chunk<kChunk>(a.rows, a.serial_len, (int)slot, lane, ok);
+  if (h == 0) {
+    if (!ok && a.status)
+      for (int64_t i = (int64_t)slot * kThreads + threadIdx.x; i < a.rows.B; i += (int64_t)space.slots * kThreads)
+        a.status[i] = SLA_ERR_LENGTH;
+    if (slot == 0 && threadIdx.x == 0) *space.walk_count() = ok ? c.longer : -1;
+    if (c.b >= 0 && c.first && wave == 0) {
+      const int place = a.rows.B <= kWave ? place_by_length(a.rows, c.b, lane) : c.rank;
+      if (lane == 0) {
+        *space.walk(place) = Walk{c.b, c.row, a.rows.start[c.b + 1] - c.row, c.row / kChunk + c.rank};
+        if (a.status) a.status[c.b] = SLA_OK;
+      }
+    }
+  }
   if (c.b < 0 || c.rows == 0) return;
 
   // keys to LDS, queries to registers, gates
@@ -435,16 +448,15 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
   const unsigned wg = workgroup(), at = wg / kXcdCount;
   const unsigned place = at / (unsigned)slabs * kXcdCount + wg % kXcdCount;
   const int slab = (int)(at % (unsigned)slabs);
-  if (place >= (unsigned)a.rows.B * (unsigned)a.H) return;
-  const int b = by_length(a.rows, (int)(place / (unsigned)a.H), lane), h = (int)(place % (unsigned)a.H), kh = h / (a.H / a.Hk);
+  if (place >= (unsigned)space.walks * (unsigned)a.H) return;
+  const int number = (int)(place / (unsigned)a.H), h = (int)(place % (unsigned)a.H), kh = h / (a.H / a.Hk);
+  if (number >= __builtin_amdgcn_readfirstlane(*space.walk_count())) return;
+  const Walk walk = *space.walk(number);
+  const int b = __builtin_amdgcn_readfirstlane(walk.b), start = __builtin_amdgcn_readfirstlane(walk.start),
+            len = __builtin_amdgcn_readfirstlane(walk.len);
   const size_t unit = (size_t)b * a.H + h;
-  const int start = __builtin_amdgcn_readfirstlane(a.rows.start[b]);
-  const int len = __builtin_amdgcn_readfirstlane(a.rows.start[b + 1]) - start;
-  const bool ok = starts_ok(a.rows, lane);
-  if (a.status && h == 0 && slab == 0 && threadIdx.x == 0) a.status[b] = ok ? SLA_OK : SLA_ERR_LENGTH;
-  if (!ok) return;
   const int chunks = (len + kChunk - 1) / kChunk, last = chunks - 1, tail = len - last * kChunk;
-  const size_t slot0 = (size_t)(start / kChunk) + b;
+  const size_t slot0 = (size_t)__builtin_amdgcn_readfirstlane(walk.slot);
   auto rows_of = [&](const void *p, int64_t stride, size_t first, int width) {
     return ChunkRows{reinterpret_cast<const unsigned char *>(static_cast<const T *>(p) + start * stride + first),
                      kChunk * stride * w, (uint32_t)((kChunk - 1) * (int)stride + width) * w,
@@ -759,7 +771,7 @@ hipError_t launch_states(const PrefillArgs &a, hipStream_t s) {
   const hipError_t e = allow_lds(second, L::kBytes);
   if (e != hipSuccess) return e;
   const int slabs = (a.dv + 16 * NT - 1) / (16 * NT);
-  const uint64_t units = ((uint64_t)a.rows.B * a.H + kXcdCount - 1) / kXcdCount * kXcdCount;
+  const uint64_t units = ((uint64_t)most_longer(a.rows, a.serial_len) * a.H + kXcdCount - 1) / kXcdCount * kXcdCount;
   hipLaunchKernelGGL(second, grid_of(units * slabs), dim3(kStateThreads), L::kBytes, s, a, slabs);
   return hipGetLastError();
 }
@@ -770,11 +782,11 @@ hipError_t launch_family(const PrefillArgs &a, hipStream_t s) {
   const auto first = matrices_kernel<F32, DK, DELTA>;
   hipError_t e = allow_lds(first, sizeof(M));
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(first, grid_of((uint64_t)chunk_slots<kChunk>(a.rows) * a.H), dim3(kThreads), sizeof(M), s, a);
+  hipLaunchKernelGGL(first, grid_of((uint64_t)chunk_slots<kChunk>(a.rows, a.serial_len) * a.H), dim3(kThreads), sizeof(M), s, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   // 16 columns of a state to a workgroup where 32 leave half of the CUs without one
-  const int64_t wide = (int64_t)a.rows.B * a.H * ((a.dv + 31) / 32);
+  const int64_t wide = most_longer(a.rows, a.serial_len) * a.H * ((a.dv + 31) / 32);
   return wide <= device_cus() / 2 ? launch_states<F32, DK, 1, DELTA>(a, s) : launch_states<F32, DK, 2, DELTA>(a, s);
 }
 

@@ -109,6 +109,13 @@ constexpr int kTriFrags = 6;
 //   power of two apart, so that a head's rows all fall to one channel of the L2; the
 //   workgroups of a head that read them chunk by chunk would wait there for one
 //   another (one sequence of 32768 tokens, 16 heads: 998 us against NNN).
+//   and behind them which sequences the second walks, the longest first in batches of
+//   up to 64, so that no long one is begun when the others have ended: their number
+//   (-1: bad starts), then one of these each.
+struct Walk {
+  int32_t b, start, len, slot;
+};
+
 template <bool F32, int DK>
 struct ChunkSpace {
   static constexpr size_t kPiece = 64 * 16;
@@ -120,17 +127,21 @@ struct ChunkSpace {
   static constexpr size_t kKeys = 3 * kRows;
 
   unsigned char *base;
-  size_t slots;
+  size_t slots, walks;
   int H, Hk;
 
-  __host__ __device__ size_t bytes() const { return slots * (H * kHead + Hk * kKeys); }
+  __host__ __device__ size_t operands() const { return slots * (H * kHead + Hk * kKeys); }
+  __host__ __device__ size_t bytes() const { return operands() + (walks + 1) * sizeof(Walk); }
+  __device__ int32_t *walk_count() const { return reinterpret_cast<int32_t *>(base + operands()); }
+  __device__ Walk *walk(int i) const { return reinterpret_cast<Walk *>(base + operands()) + 1 + i; }
   __device__ unsigned char *head(size_t slot, int h) const { return base + (slot * H + h) * kHead; }
   __device__ unsigned char *keys(size_t slot, int kh) const { return base + slots * H * kHead + (slot * Hk + kh) * kKeys; }
 };
 
 template <bool F32, int DK>
 __host__ __device__ inline ChunkSpace<F32, DK> chunk_space(const PrefillArgs &a) {
-  return {static_cast<unsigned char *>(a.workspace), (size_t)chunk_slots<kChunk>(a.rows), a.H, a.Hk};
+  return {static_cast<unsigned char *>(a.workspace), (size_t)chunk_slots<kChunk>(a.rows, a.serial_len),
+          (size_t)most_longer(a.rows, a.serial_len), a.H, a.Hk};
 }
 
 // Each returns hipSuccess or the launch error (specialised in prefill_chunk.hip's units).

@@ -21,6 +21,7 @@ struct PrefillArgs {
   PackedRows rows;
   int32_t H, Hk, dk, dv;
   int32_t family;
+  int32_t serial_len;    // sequences up to this length go token by token, longer ones in chunks (-1: all in chunks)
   const float *state;    // [B][H][dk][dv] or null
   const void *q, *k, *v;
   int64_t q_stride, k_stride, v_stride;  // elements from row to row

@@ -14,37 +14,39 @@ __device__ __forceinline__ void store4(float *p, const float (&x)[4]) {
   *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
 }
 
-// Whether the starts are in order and inside the rows (wave-uniform).  Every
-// wave looks at all of them: the loads are independent, 64 sequences at a time.
+// Sequences longer than min_len (-1: all) there can be.
+__host__ __device__ inline int64_t most_longer(const PackedRows &r, int min_len) {
+  const int64_t most = min_len < 0 ? r.B : r.tokens / (min_len + 1);
+  return most < r.B ? most : r.B;
+}
+
+// Chunks of C tokens of the sequences longer than min_len (-1: of all, an empty one
+// having one empty chunk).  Chunk c of sequence b has the slot start[b] / C + rank + c,
+// rank counting the longer sequences before b: ceil(len / C) <= end / C - start / C + 1,
+// so no two share one, and no table of chunk counts has to be summed up first.  Some
+// slots stay empty.
+template <int C>
+__host__ __device__ inline int64_t chunk_slots(const PackedRows &r, int min_len) {
+  return (int64_t)r.tokens / C + most_longer(r, min_len);
+}
+
+// Whether the starts are in order and inside the rows (wave-uniform).  Every wave
+// looks at all of them: the loads are independent, 64 sequences at a time.
 __device__ __forceinline__ bool starts_ok(const PackedRows &r, int lane) {
   bool bad = false;
   for (int i = lane; i < r.B; i += kWave) {
-    const int a = r.start[i], b = r.start[i + 1];
-    bad = bad || a < 0 || a > b || b > r.tokens;
+    const int a = r.start[i], e = r.start[i + 1];
+    bad = bad || a < 0 || a > e || e > r.tokens;
   }
   return !wave_any(bad);
 }
 
-// Chunks of C tokens.  Sequence b's chunk c has the slot start[b] / C + b + c:
-// ceil(len / C) <= end / C - start / C + 1, so no two share one, and no table of
-// chunk counts has to be summed up first.  Some slots stay empty.
-template <int C>
-__host__ __device__ inline int64_t chunk_slots(const PackedRows &r) {
-  return (int64_t)r.tokens / C + r.B;
-}
-
-// The sequence to be begun as number `place`: the longest first, for batches of up
-// to 64, so that no long one is begun when the others have ended; else in order.
-// (Wave-uniform; starts need not be in order.)
-__device__ __forceinline__ int by_length(const PackedRows &r, int place, int lane) {
-  if (r.B > kWave) return place;
-  const int len = lane < r.B ? r.start[lane + 1] - r.start[lane] : 0;
-  int rank = lane < r.B ? 0 : -1;
-  for (int i = 0; i < r.B; ++i) {
-    const int other = __builtin_amdgcn_readlane(len, i);
-    rank += lane < r.B && (other > len || (other == len && i < lane));
-  }
-  return __builtin_ctzll(__ballot(rank == place));
+// How many sequences are longer than sequence b, or as long and before it, in a batch
+// of up to 64 (wave-uniform).
+__device__ __forceinline__ int place_by_length(const PackedRows &r, int b, int lane) {
+  const int len = lane < r.B ? r.start[lane + 1] - r.start[lane] : -1;
+  const int mine = __builtin_amdgcn_readlane(len, b);
+  return __popcll(__ballot(len > mine || (len == mine && lane < b)));
 }
 
 struct Chunk {
@@ -52,33 +54,40 @@ struct Chunk {
   int row;    // first row
   int rows;   // 1..C, 0: the one chunk of an empty sequence
   bool first, last;
+  int rank;    // longer sequences before its own
+  int longer;  // longer sequences in all
 };
 
-// The chunk of a slot, of starts that are in order (wave-uniform): b is the
-// last sequence whose first slot is not behind it, counted as in starts_ok.
-// `ok` says whether the starts are in order.
+// The chunk of a slot (wave-uniform): its sequence is the last whose first slot is
+// not behind it.  `ok` says whether the starts are in order.
 template <int C>
-__device__ __forceinline__ Chunk find_chunk(const PackedRows &r, int slot, int lane, bool &ok) {
+__device__ __forceinline__ Chunk find_chunk(const PackedRows &r, int min_len, int slot, int lane, bool &ok) {
   bool bad = false;
-  int before = 0, a = 0, e = 0;
-  for (int i = lane; i - lane < r.B; i += kWave) {
-    const bool live = i < r.B;
-    a = live ? r.start[i] : 0;
-    e = live ? r.start[i + 1] : 0;
+  int rank = 0, b = -1, start = 0, end = 0, front = 0;
+  for (int i = 0; i < r.B; i += kWave) {
+    const bool live = i + lane < r.B;
+    const int a = live ? r.start[i + lane] : 0, e = live ? r.start[i + lane + 1] : 0;
     bad = bad || (live && (a < 0 || a > e || e > r.tokens));
-    before += __popcll(__ballot(live && a / C + i <= slot));
+    const uint64_t longer = __ballot(live && (int64_t)e - a > min_len);
+    const int mine = a / C + rank + __popcll(longer & ((1ull << lane) - 1));
+    const uint64_t before = __ballot(mine <= slot) & longer;
+    if (before) {
+      const int l = 63 - __builtin_clzll(before);
+      b = i + l;
+      start = __builtin_amdgcn_readlane(a, l);
+      end = __builtin_amdgcn_readlane(e, l);
+      front = __builtin_amdgcn_readlane(mine, l);
+    }
+    rank += __popcll(longer);
   }
   ok = !wave_any(bad);
-  Chunk c = {-1, 0, 0, false, false};
-  if (!ok || before == 0) return c;
-  // (the last 64 sequences' starts are at hand)
-  const int b = before - 1, kept = b - (r.B - 1) / kWave * kWave;
-  const int start = kept >= 0 ? __shfl(a, kept) : r.start[b], end = kept >= 0 ? __shfl(e, kept) : r.start[b + 1];
-  const int at = slot - (start / C + b);
-  if (at > 0 && (int64_t)at * C >= end - start) return c;
-  c.b = __builtin_amdgcn_readfirstlane(b);
-  c.row = __builtin_amdgcn_readfirstlane(start + at * C);
-  c.rows = __builtin_amdgcn_readfirstlane(min(C, end - c.row));
+  Chunk c = {-1, 0, 0, false, false, 0, rank};
+  const int at = slot - front;
+  if (!ok || b < 0 || (at > 0 && (int64_t)at * C >= end - start)) return c;
+  c.b = b;
+  c.rank = front - start / C;
+  c.row = start + at * C;
+  c.rows = min(C, end - c.row);
   c.first = at == 0;
   c.last = c.row + c.rows == end;
   return c;

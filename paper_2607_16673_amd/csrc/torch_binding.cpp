@@ -651,8 +651,8 @@ PyObject *conv_prefill(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-// recurrent_inputs(q, k, a | None, b | None, a_log | None, dt_bias | None, q_out, k_out, alpha | None, beta | None, q_scale,
-//                  eps)
+// recurrent_inputs(q, k, a | None, b | None, a_log | None, dt_bias | None, q_out, k_out, alpha | None, beta | None,
+//                  q_scale | None, eps)
 PyObject *recurrent_inputs(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   count_args(nargs, 12);
@@ -669,7 +669,7 @@ PyObject *recurrent_inputs(PyObject *, PyObject *const *o, Py_ssize_t nargs) {
   shape.repeat = size32(oh / kh, "repeat");
   shape.d_k = size32(dk, "d_k");
   shape.dtype = activation_code(q);
-  shape.q_scale = real(o[10]);
+  shape.q_scale = o[10] == Py_None ? (float)(1.0 / std::sqrt((double)dk)) : real(o[10]);
   shape.eps = real(o[11]);
   const Packed r(q);
   int64_t qs, ks, as = H, bs = H;
