@@ -4,12 +4,12 @@ cache, random weights, greedy sampling.
 
     python examples/hybrid_round.py [--tokens 64] [--branches 4] [--plain]
 
-A prompt is run once, in chunks of 64 nodes; its sequence forks into branches
-that go on from the prompt's likeliest next tokens and share its pages.  In a
-round every branch drafts a tree, looked up in its own text, all layers verify
-the trees in one pass, and the accepted paths are committed: the recurrent and
-convolution states of every layer, and the cache rows of all attention layers in
-one call.  --plain decodes one token a round instead; the tokens are the same.
+A prompt is run once: the recurrent layers take all its tokens in one call, the
+attention layers chunks of 64 nodes.  Its sequence forks into branches that go on
+from the prompt's likeliest next tokens and share its pages.  In a round every
+branch drafts a tree, looked up in its own text, all layers verify the trees in
+one pass, and the accepted paths are committed: the recurrent and convolution
+states of every layer, and the cache rows of all attention layers in one call.  --plain decodes one token a round instead; the tokens are the same.
 """
 from __future__ import annotations
 
@@ -76,6 +76,19 @@ class Session:
         s.conv = [x.repeat(batch, 1, 1) for x in self.conv]
         return s
 
+    def unit_heads(self, rows):
+        """Convolved rows as queries and keys of length 1, and values."""
+        q, k, v = (p.unflatten(1, (R_HEADS, R_HEAD)) for p in rows.split(R_HEADS * R_HEAD, 1))
+        unit = [torch.empty(q.shape, dtype=q.dtype, device="cuda") for _ in "qk"]
+        sla.sla_recurrent_inputs(q, k, None, None, None, None, *unit, None, None, q_scale=1.0, eps=1e-12)
+        return *unit, v
+
+    def norm_heads(self, o):
+        """The recurrence's output, normalised head by head, in the weights' type."""
+        y = torch.empty(o.shape, dtype=self.t.dtype, device="cuda")
+        sla.sla_gated_norm(o, None, None, y, gate="none")
+        return y
+
     def verify(self, tokens, parent):
         """Logits [B][n][VOCAB] of every draft node; nothing is committed yet."""
         t, B, n = self.t, self.B, tokens.shape[1]
@@ -96,15 +109,14 @@ class Session:
             u, gates = h @ w["qkv"], (h @ w["gates"]).float().sigmoid()
             y = torch.empty_like(u)
             sla.sla_conv_verify(self.conv[i], u, w["taps"], self.parent, y, status=self.status[3 * i])
-            q, k, v = (p.unflatten(2, (R_HEADS, R_HEAD)) for p in y.split(R_HEADS * R_HEAD, 2))
-            q, k = (torch.nn.functional.normalize(p.float(), dim=-1).to(t.dtype) for p in (q, k))
+            q, k, v = self.unit_heads(y.flatten(0, 1))
             alpha, beta = (p.contiguous() for p in (0.9 + 0.1 * gates[..., :R_HEADS], gates[..., R_HEADS:]))
             o = torch.empty(B, n, R_HEADS, R_HEAD, device="cuda")
             factors = sla.Factors.empty(B, n, R_HEADS, R_HEAD, R_HEAD, t.dtype)
-            sla.sla_verify(self.state[i], q, k, v.contiguous(), alpha, beta, self.parent, o, factors,
-                           status=self.status[3 * i + 1])
+            sla.sla_verify(self.state[i], q.unflatten(0, (B, n)), k.unflatten(0, (B, n)), v.contiguous().unflatten(0, (B, n)),
+                           alpha, beta, self.parent, o, factors, status=self.status[3 * i + 1])
             self.kept.append((u, factors))
-            x = x + (unit_rms(o).flatten(2).to(t.dtype) @ w["out"]).float()
+            x = x + (self.norm_heads(o.flatten(0, 1)).unflatten(0, (B, n)).flatten(2) @ w["out"]).float()
             # attention: one fused projection, norms and rotation on the way into the cache
             qkv = (unit_rms(x).to(t.dtype) @ w["attn_qkv"]).unflatten(2, (-1, HEAD))
             q, k, v = qkv.split([HEADS, KV_HEADS, KV_HEADS], 2)
@@ -131,13 +143,54 @@ class Session:
             s.length += int(k)
 
     def prompt(self, tokens):
-        """Run a prompt (the same in every sequence); returns the last token's logits."""
-        for i in range(0, len(tokens), CHUNK):
-            part = np.tile(np.asarray(tokens[i:i + CHUNK], np.int32), (self.B, 1))
-            chain = np.tile(np.arange(-1, part.shape[1] - 1, dtype=np.int32), (self.B, 1))
-            logits = self.verify(part, chain)
-            self.commit(chain + 1, np.full(self.B, part.shape[1], np.int32))
-        return logits[:, -1]
+        """Run a prompt (the same in every sequence) and commit it; returns the last token's logits."""
+        t, B, T = self.t, self.B, len(tokens)
+        copies = self.pool.reserve_all(self.seqs, T)
+        if copies:
+            src, dst, rows = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in zip(*copies))
+            sla.sla_page_copy(*self.cache, src, dst, rows=rows)
+        table = torch.from_numpy(self.pool.table(self.seqs)).cuda()
+        base = torch.tensor([s.length for s in self.seqs], dtype=torch.int32, device="cuda")
+        start = torch.arange(B + 1, dtype=torch.int32, device="cuda") * T
+        status = torch.zeros(BLOCKS, 2, B, dtype=torch.int32, device="cuda")
+        # an attention layer's chunks: (first token, nodes, chunks), the last one shorter
+        full = T // CHUNK
+        parts = [p for p in ((0, CHUNK, full), (full * CHUNK, T - full * CHUNK, 1)) if p[1] * p[2]]
+        x = t.embed[torch.from_numpy(np.asarray(tokens)).long().cuda()].repeat(B, 1)  # [B T][WIDTH]
+        for i, w in enumerate(t.layers):
+            h = unit_rms(x).to(t.dtype)
+            u, gates = h @ w["qkv"], (h @ w["gates"]).float().sigmoid()
+            y = torch.empty_like(u)
+            sla.sla_conv_prefill(u, w["taps"], start, y, self.conv[i], conv_state=self.conv[i], status=status[i, 0])
+            q, k, v = self.unit_heads(y)
+            alpha, beta = (p.contiguous() for p in (0.9 + 0.1 * gates[:, :R_HEADS], gates[:, R_HEADS:]))
+            o = torch.empty(v.shape, dtype=v.dtype, device="cuda")
+            sla.sla_prefill(q, k, v, alpha, beta, start, o, self.state[i], state=self.state[i],
+                            workspace=sla.prefill_workspace(q, v, B), status=status[i, 1])
+            x = x + (self.norm_heads(o).flatten(1) @ w["out"]).float()
+            qkv = (unit_rms(x).to(t.dtype) @ w["attn_qkv"]).view(B, T, -1, HEAD)
+            o = torch.empty(B, T, HEADS, HEAD, dtype=t.dtype, device="cuda")
+            for first, n, chunks in parts:
+                q, k, v = qkv[:, first:first + n * chunks].reshape(B * chunks, n, -1, HEAD).split([HEADS, KV_HEADS, KV_HEADS], 2)
+                chain = torch.arange(-1, n - 1, dtype=torch.int32, device="cuda").repeat(B * chunks, 1)
+                rows = table.repeat_interleave(chunks, 0)
+                lens = (base[:, None] + first + n * torch.arange(chunks, device="cuda")).flatten().int()
+                turned = torch.empty(q.shape, dtype=t.dtype, device="cuda")
+                k_cache, v_cache = (c[i] for c in self.cache)
+                errors = torch.zeros(B * chunks, dtype=torch.int32, device="cuda")
+                sla.sla_attn_append(q, k, v, chain, rows, lens, turned, k_cache, v_cache, q_norm=w["q_norm"],
+                                    k_norm=w["k_norm"], rope=t.rope, status=errors, topology="chain")
+                seen = torch.empty_like(turned)
+                sla.sla_attn_verify(turned, k_cache, v_cache, chain, rows, lens, seen, topology="chain",
+                                    workspace=sla.attn_workspace(turned, k_cache, rows))
+                o[:, first:first + n * chunks] = seen.view(B, n * chunks, HEADS, HEAD)
+                status[i, 0] += errors.view(B, chunks).sum(1).int()
+            x = x + (o.view(B * T, -1) @ w["attn_out"]).float()
+        if status.any():
+            raise RuntimeError("a sequence's data are bad: %s" % status.tolist())
+        for s in self.seqs:
+            s.length += T
+        return (unit_rms(x.view(B, T, -1)[:, -1]).to(t.dtype) @ t.head).float()
 
     def close(self):
         for s in self.seqs:

@@ -141,14 +141,18 @@ hipError_t launch_serial(const PrefillArgs &a, hipStream_t s) {
 
 // Which sequences go token by token: a chunk takes the chunked kernels about as long
 // whether it is full or not.  16 heads of 128, microseconds token by token and in
-// chunks: one sequence of 6 tokens 11.8 and 13.7, of 8 tokens 14.7 and 13.7; 256
-// sequences, whose states fill the chip, of 4 tokens 126 and 452, of 24 tokens 388 and
-// 464.  Where all tokens together are no more, one launch does; where there are 64 a
-// sequence, all go in chunks, without the launch for short ones among them.
+// chunks: one sequence of 6 tokens 11.9 and 13.7, of 8 tokens 14.7 and 13.7; 8
+// sequences of 6 tokens 18.1 and 21.6; 256 sequences, whose states fill the chip, of 4
+// tokens 126 and 452, of 24 tokens 388 and 464.  Lengths are on the device: each kernel
+// passes over the others' sequences, and a launch that may find none of its own costs
+// 3 us.  So where all tokens together are few enough for one sequence, one launch does;
+// where an average sequence is long (few workgroups: longer than the limit; many: 64
+// tokens) all go in chunks, and short ones among them cost little beside the others.
 PrefillArgs divided(PrefillArgs a) {
   const int64_t workgroups = (int64_t)a.rows.B * a.H * ((a.dv + kCols - 1) / kCols);
-  a.serial_len = workgroups >= 4 * device_cus() ? 24 : 6;
-  if (a.rows.tokens >= 64 * (int64_t)a.rows.B) a.serial_len = -1;
+  const bool fills = workgroups >= 4 * device_cus();
+  a.serial_len = fills ? 24 : 6;
+  if (a.rows.tokens > (fills ? 64 : 6) * (int64_t)a.rows.B) a.serial_len = -1;
   return a;
 }
 bool all_serial(const PrefillArgs &a) { return a.rows.tokens <= a.serial_len; }

@@ -53,7 +53,7 @@ struct Chunk {
   int b;      // sequence, -1: none
   int row;    // first row
   int rows;   // 1..C, 0: the one chunk of an empty sequence
-  bool first, last;
+  bool first;
   int rank;    // longer sequences before its own
   int longer;  // longer sequences in all
 };
@@ -81,7 +81,7 @@ __device__ __forceinline__ Chunk find_chunk(const PackedRows &r, int min_len, in
     rank += __popcll(longer);
   }
   ok = !wave_any(bad);
-  Chunk c = {-1, 0, 0, false, false, 0, rank};
+  Chunk c = {-1, 0, 0, false, 0, rank};
   const int at = slot - front;
   if (!ok || b < 0 || (at > 0 && (int64_t)at * C >= end - start)) return c;
   c.b = b;
@@ -89,7 +89,6 @@ __device__ __forceinline__ Chunk find_chunk(const PackedRows &r, int min_len, in
   c.row = start + at * C;
   c.rows = min(C, end - c.row);
   c.first = at == 0;
-  c.last = c.row + c.rows == end;
   return c;
 }
 
