@@ -368,8 +368,7 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
 // neighbouring columns of a token.
 template <bool F32, int DK, int NT>
 struct StateLds {
-  static constexpr int kPieces = kPiecesOf<F32, kStatePlanes>;
-  static constexpr int kOutPieces = kPiecesOf<F32, kOutPlanes>;
+  static constexpr int kPieces = kStatePlanes, kOutPieces = F32 ? kStatePlanes : kOutPlanes;
   static constexpr size_t kFrag = (size_t)kPieces * kWave * 16, kOutFrag = (size_t)kOutPieces * kWave * 16;
   static constexpr int kStateFrags = DK / 32 * NT, kRowFrags = 2 * NT;
   // H, V - G o (K H), D_63 o U, U
@@ -377,24 +376,20 @@ struct StateLds {
 };
 
 // half `half` (4 of 8 values) of a lane's operand
-template <bool F32, int N>
+template <int N>
 __device__ __forceinline__ void put_half(unsigned char *frag, int half, int lane, f32x4 x) {
-  if constexpr (F32) {
-    *reinterpret_cast<f32x4 *>(frag + (half * kWave + lane) * 16) = x;
-  } else {
-    const float v[4] = {x[0], x[1], x[2], x[3]};
-    uint2 p[N];
-    split4(v, p);
+  const float v[4] = {x[0], x[1], x[2], x[3]};
+  uint2 p[N];
+  split4(v, p);
 #pragma unroll
-    for (int n = 0; n < N; ++n) *reinterpret_cast<uint2 *>(frag + (n * kWave + lane) * 16 + 8 * half) = p[n];
-  }
+  for (int n = 0; n < N; ++n) *reinterpret_cast<uint2 *>(frag + (n * kWave + lane) * 16 + 8 * half) = p[n];
 }
 
-template <bool F32, int N>
-__device__ __forceinline__ Frag<F32, N> get_frag(const unsigned char *frag, int lane) {
-  Frag<F32, N> f;
+template <int N>
+__device__ __forceinline__ Frag<false, N> get_frag(const unsigned char *frag, int lane) {
+  Frag<false, N> f;
 #pragma unroll
-  for (int n = 0; n < kPiecesOf<F32, N>; ++n) f.p[n] = *reinterpret_cast<const typename Frag<F32, N>::Piece *>(frag + (n * kWave + lane) * 16);
+  for (int n = 0; n < N; ++n) f.p[n] = *reinterpret_cast<const bf16x8 *>(frag + (n * kWave + lane) * 16);
   return f;
 }
 
@@ -416,9 +411,9 @@ __device__ __forceinline__ void pace() {
   if constexpr (F + 1 < FRAGS) pace<AHEAD, R, M, FRAGS, LOADS, F + 1>();
 }
 
-// matrix instructions of one product of N planes
+// matrix instructions of one product of N planes with an activation
 template <bool F32, int N>
-constexpr int kMfma = F32 ? 8 : N;
+constexpr int kMfma = F32 ? 6 : N;
 
 constexpr int kStateThreads = 512;
 // of the state kernel: two workgroups to a CU where their registers hold the operands
@@ -448,7 +443,8 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
   using Piece = typename Frag<F32, 1>::Piece;
   constexpr int kKs = DK / 32, kTiles = DK / 64, w = sizeof(T);
   constexpr int kKeyPieces = kPiecesOf<F32, 1>, kStatePieces = kPiecesOf<F32, kStatePlanes>, kOutPieces = kPiecesOf<F32, kOutPlanes>;
-  constexpr int kParts = NT == 1 ? (F32 ? 2 : 3) : 1, kOutParts = NT == 1 ? 2 : 1;
+  constexpr int kActs = F32 ? 3 : 1, kOuts = L::kOutPieces;  // planes of an activation, and for outputs
+  constexpr int kParts = NT == 1 ? 3 : 1, kOutParts = NT == 1 ? 2 : 1;
   constexpr bool kTouch = kWavesPerSimd<F32, DK, NT> == 2;
   constexpr bool kTwoSets = NT == 1 && DK <= (F32 ? 64 : 128);
   constexpr int kAhead = NT == 1 ? 8 : 2;  // of the state's operands read in front of their products
@@ -554,7 +550,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
     auto put_state = [&](int m) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
-        put_half<F32, kStatePlanes>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
+        put_half<kStatePlanes>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
     };
 
     // One chunk, from the operands `x`; the next one's go to `y`.  Where registers
@@ -571,7 +567,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            sum[n].template add<1, kStatePlanes>(x.kf[ks], get_frag<F32, kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane));
+            sum[n].template add<kActs, kStatePlanes>(planes(x.kf[ks]), get_frag<kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane));
         if (kTwoSets) {
           load_k(y, keys);
           load_v(y, c + 1, head);
@@ -591,7 +587,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
           const float v = __uint_as_float(F32 ? x.vr[n][i] : x.vr[n][i] << 16);
           u[n][i] = DELTA ? __builtin_fmaf(-x.gr[i], u[n][i], v) : v;
         }
-        if (DELTA) put_half<F32, kStatePlanes>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, u[n]);
+        if (DELTA) put_half<kStatePlanes>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, u[n]);
       }
       if (!kTwoSets) load_v(y, c + 1, head);
       if constexpr (DELTA) {
@@ -601,12 +597,12 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            sum[n].template add<kStatePlanes, kStatePlanes>(x.ts[ks], get_frag<F32, kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane));
+            sum[n].template add<kStatePlanes, kStatePlanes>(planes(x.ts[ks]), get_frag<kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane));
         if (kTwoSets) {
           load_matrix(y, head);
           load_decay(y, head);
         }
-        pace<2, L::kPieces, F32 ? 8 : 6, 2 * NT, kTwoSets ? kSolveLoads : 0>();
+        pace<2, L::kPieces, 6, 2 * NT, kTwoSets ? kSolveLoads : 0>();
         __builtin_amdgcn_sched_barrier(0);
         if (!kTwoSets) load_matrix(y, head);
 #pragma unroll
@@ -616,8 +612,8 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        put_half<F32, kStatePlanes>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, x.gu * u[n]);
-        put_half<F32, kOutPlanes>(lds_o + (size_t)(wave / 2 * NT + n) * L::kOutFrag, half, lane, u[n]);
+        put_half<kStatePlanes>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, x.gu * u[n]);
+        put_half<kOuts>(lds_o + (size_t)(wave / 2 * NT + n) * L::kOutFrag, half, lane, u[n]);
       }
       const float whole = x.gc;
       if (!kTwoSets) load_decay(y, head);
@@ -631,9 +627,9 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const Frag<F32, kStatePlanes> uf = get_frag<F32, kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
+          const Frag<false, kStatePlanes> uf = get_frag<kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
 #pragma unroll
-          for (int m = 0; m < kTiles; ++m) next[m][n].template add<1, kStatePlanes>(x.key[m][ks], uf);
+          for (int m = 0; m < kTiles; ++m) next[m][n].template add<kActs, kStatePlanes>(planes(x.key[m][ks]), uf);
         }
       if (kTwoSets) load_keys(y, keys);
       pace<2, L::kPieces, kTiles * kMfma<F32, 3>, 2 * NT, kTwoSets ? kKeyLoads : 0>();
@@ -735,8 +731,8 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          sum[n].template add<kOutPlanes, 1>(get_frag<F32, kOutPlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane), qf[ks]);
-      pace<kAhead, kOutPieces, kMfma<F32, 2>, kKs * NT>();
+          sum[n].template add<kOuts, kActs>(get_frag<kOuts>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane), planes(qf[ks]));
+      pace<kAhead, kOuts, kMfma<F32, 2>, kKs * NT>();
       __builtin_amdgcn_sched_barrier(0);
       load_q(c + 1);
       if (DELTA) lds_barrier();
@@ -749,7 +745,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          sum[n].template add<kOutPlanes, kOutPlanes>(get_frag<F32, kOutPlanes>(lds_o + (size_t)(ks * NT + n) * L::kOutFrag, lane), to[ks]);
+          sum[n].template add<kOuts, kOuts>(get_frag<kOuts>(lds_o + (size_t)(ks * NT + n) * L::kOutFrag, lane), planes(to[ks]));
       f32x4 o[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n) o[n] = sum[n].total();

@@ -25,7 +25,8 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 // index of row `r` of tile `t`
 __host__ __device__ constexpr int tile_row(int t, int r) { return 32 * (t / 2) + 8 * (r / 4) + 4 * (t % 2) + r % 4; }
 
-// An operand: N bf16 planes, 8 bits of the values each, or fp32 values.
+// An operand: N bf16 planes, 8 bits of the values each, or fp32 values (as they lie in
+// memory; see `planes`).
 template <bool F32, int N>
 struct Frag {
   using Piece = bf16x8;
@@ -39,6 +40,40 @@ struct Frag<true, N> {
 // 16-byte pieces of a lane
 template <bool F32, int N>
 constexpr int kPiecesOf = F32 ? 2 : N;
+
+// The bf16 planes of 4 values: the leading 8 bits of each, the next 8, the last
+// 8 (cut, not rounded: three planes are the value itself, and a mask and a
+// subtraction cost less than a conversion).
+template <int N>
+__device__ __forceinline__ void split4(const float (&x)[4], uint2 (&p)[N]) {
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(x[i]);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    p[n] = make_uint2(__builtin_amdgcn_perm(r[1], r[0], 0x07060302u), __builtin_amdgcn_perm(r[3], r[2], 0x07060302u));
+    if (n + 1 < N)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) - __uint_as_float(r[i] & 0xffff0000u));
+  }
+}
+
+// An operand of the second kernel as bf16 planes.  Six products of those of fp32 values
+// take 96 cycles where eight fp32 instructions take 256, and leave out 2^-24 of a
+// product's size at most, as a rounding of it would.
+template <int N>
+__device__ __forceinline__ const Frag<false, N> &planes(const Frag<false, N> &f) { return f; }
+template <int N>
+__device__ __forceinline__ Frag<false, 3> planes(const Frag<true, N> &f) {
+  const float lo[4] = {f.p[0][0], f.p[0][1], f.p[0][2], f.p[0][3]}, hi[4] = {f.p[1][0], f.p[1][1], f.p[1][2], f.p[1][3]};
+  uint2 a[3], b[3];
+  split4(lo, a);
+  split4(hi, b);
+  Frag<false, 3> s;
+#pragma unroll
+  for (int n = 0; n < 3; ++n) s.p[n] = __builtin_bit_cast(bf16x8, make_uint4(a[n].x, a[n].y, b[n].x, b[n].y));
+  return s;
+}
 
 // A sum of products a b of the first NA and NB planes, those of 2^-8 max(NA, NB)
 // and less of the whole left out.  It is held in S parts, by the products' size: a
@@ -76,25 +111,8 @@ struct Sum {
   }
 };
 
-// The bf16 planes of 4 values: the leading 8 bits of each, the next 8, the last
-// 8 (cut, not rounded: three planes are the value itself, and a mask and a
-// subtraction cost less than a conversion).
-template <int N>
-__device__ __forceinline__ void split4(const float (&x)[4], uint2 (&p)[N]) {
-  uint32_t r[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(x[i]);
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    p[n] = make_uint2(__builtin_amdgcn_perm(r[1], r[0], 0x07060302u), __builtin_amdgcn_perm(r[3], r[2], 0x07060302u));
-    if (n + 1 < N)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) - __uint_as_float(r[i] & 0xffff0000u));
-  }
-}
-
-// Planes of what the state depends on, and of what outputs alone do, which are
-// rounded to bf16.
+// Planes of what the state depends on, and of what outputs alone do that are rounded
+// to bf16.
 constexpr int kStatePlanes = 3, kOutPlanes = 2;
 
 // Row tile t of the lower triangular 64 x 64 matrices has the inner 32s ks <= t / 2.
