@@ -485,6 +485,12 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
     int col[NT];  // this lane's columns as an operand's row
 #pragma unroll
     for (int n = 0; n < NT; ++n) col[n] = slab * 16 * NT + (NT == 1 ? r : 32 * (n / 2) + 8 * (r / 4) + 4 * (n % 2) + r % 4);
+    // the state's row i of tile m is at h_off + (64 m + i) rows (columns past its own, and no state, read as zeros)
+    uint32_t h_off[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) h_off[n] = col[n] < a.dv ? (uint32_t)(tile_row(wave, 4 * g) * a.dv + col[n]) * 4 : kNowhere;
+    const size_t state_at = unit * DK * a.dv;
+    const rsrc_t state_in = make_rsrc(a.state ? a.state + state_at : nullptr, a.state ? (uint32_t)DK * a.dv * 4 : 0u);
     f32x4 H[kTiles][NT];
 #pragma unroll
     for (int m = 0; m < kTiles; ++m)
@@ -492,8 +498,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          H[m][n][i] = a.state && col[n] < a.dv
-                           ? a.state[(unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] : 0.f;
+          H[m][n][i] = buf_load_f32<kPolicyDefault>(state_in, h_off[n], (uint32_t)((64 * m + i) * a.dv) * 4);
 
     ChunkRows v_rows = rows_of(a.v, a.v_stride, (size_t)h * a.dv, a.dv);
     uint32_t v_off[NT];
@@ -668,13 +673,14 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
     } else {
       for (int c = 0; c < chunks; ++c) step(c, even, even);
     }
+    const rsrc_t state_out = make_rsrc(a.state_out + state_at, (uint32_t)DK * a.dv * 4);
 #pragma unroll
     for (int m = 0; m < kTiles; ++m)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (col[n] < a.dv) a.state_out[(unit * DK + tile_row(wave + 4 * m, 4 * g + i)) * a.dv + col[n]] = H[m][n][i];
+          buf_store_f32<kPolicyDefault>(H[m][n][i], state_out, h_off[n], (uint32_t)((64 * m + i) * a.dv) * 4);
   } else {
     // lane: token 16 wave + r, columns 4 g + i of each tile
     const int token = 16 * wave + r;
