@@ -554,8 +554,8 @@ int sla_page_copy(const sla_attn_shape *shape, int32_t layers, void *k_cache, vo
  * and z multiples of 16 bytes and of at most 2^22 elements, else
  * SLA_ERR_UNSUPPORTED.  With no rows (tokens = 0, rows = 0) the pointers to
  * rows may be NULL.  Results are the same from run to run, and a sequence's do
- * not depend on the others of its batch, but for the last bits of sla_prefill of
- * short sequences, which go by the call's rows and sequences. */
+ * not depend on the others of its batch, but for the last bits of sla_prefill's,
+ * which go by the call's sizes as the division of its work does. */
 
 typedef struct sla_prefill_shape {
   int32_t tokens;    /* rows T of q, k, v and out, 0..2^30                     */
@@ -584,10 +584,11 @@ typedef struct sla_prefill_shape {
  *             finished; it needs no initialisation.
  *   status    device int32 [B] or NULL: 0 or SLA_ERR_LENGTH.
  * Gates are only multiplied, so any in the range, however small, is valid.
- * Sums and states are fp32; bf16 activations are read exactly, products with
- * fp32 values keep 24 bits of those for the state, and 16 for the output, which
- * is rounded to bf16.  A NaN or an infinity in a sequence's rows spoils all its
- * outputs from the first one of its chunk of 64 tokens on, and its state. */
+ * Sums and states are fp32; bf16 activations are read exactly.  fp32 values enter
+ * products with 24 bits, or with 16 where nothing but an output that is rounded
+ * to bf16 depends on the product.  A NaN or an infinity in a sequence's rows
+ * spoils all its outputs from the first one of its chunk of 64 tokens on, and its
+ * state. */
 int sla_prefill(const sla_prefill_shape *shape, const float *state, const void *q, int64_t q_stride,
                 const void *k, int64_t k_stride, const void *v, int64_t v_stride, const float *alpha,
                 const float *beta, const int32_t *seq_start, void *out, float *state_out, void *workspace,
