@@ -359,8 +359,8 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
 //
 // The chain of chunks bounds one long sequence: 512 chunks, 16 heads of 128, 815 us or
 // 3800 cycles a chunk, of which three products from LDS, their planes cut and put back
-// and the barriers are 2900, the rest waits for loads (870 us without `touch` below; 532
-// with no loads).  Many sequences are bound by LDS, matrix cores and vector ALUs in
+// and the barriers are 2900, the rest waits for loads (870 us without `touch` below, 617
+// with every chunk's lines the same, 532 with no loads).  Many sequences are bound by LDS, matrix cores and vector ALUs in
 // turn (53, 40 and 39% busy): 32 sequences of up to 2048 tokens, 32 heads, 537 chunks
 // in 588 us with two workgroups to a CU.  Four column tiles to a workgroup take 653,
 // one takes 860.  fp32 activations are bound by the vector ALUs, busy 60%, which cut
