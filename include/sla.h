@@ -584,11 +584,12 @@ typedef struct sla_prefill_shape {
  *             finished; it needs no initialisation.
  *   status    device int32 [B] or NULL: 0 or SLA_ERR_LENGTH.
  * Gates are only multiplied, so any in the range, however small, is valid.
- * Sums and states are fp32; bf16 activations are read exactly.  fp32 values enter
- * products with 24 bits, or with 16 where nothing but an output that is rounded
- * to bf16 depends on the product.  A NaN or an infinity in a sequence's rows
- * spoils all its outputs from the first one of its chunk of 64 tokens on, and its
- * state. */
+ * Sums and states are fp32 and bf16 activations are read exactly.  A product leaves
+ * out 2^-24 of its size at most, as a rounding of it would; outputs are rounded to
+ * bf16 once.  Magnitudes of 3.3961e38 or more (they round past the largest bf16)
+ * count as infinite.  A NaN or an infinity in a sequence's rows may spoil its outputs
+ * from the first one of its chunk of 64 tokens on, and its state; none before that,
+ * and no other sequence's. */
 int sla_prefill(const sla_prefill_shape *shape, const float *state, const void *q, int64_t q_stride,
                 const void *k, int64_t k_stride, const void *v, int64_t v_stride, const float *alpha,
                 const float *beta, const int32_t *seq_start, void *out, float *state_out, void *workspace,

@@ -229,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
       if (ks <= wave / 2)
-        store_frag<F32, kOutPlanes>(head + space.kSolve + (size_t)(first_frag(wave) + ks) * kPiecesOf<F32, kOutPlanes> * space.kPiece, lane, p[ks]);
+        store_frag<true, kPlanes>(head + space.kSolve + (size_t)(first_frag(wave) + ks) * kPiecesOf<true, kPlanes> * space.kPiece, lane, p[ks]);
   }
   if (threadIdx.x < kChunk) {
     reinterpret_cast<float *>(head + space.kDecay)[threadIdx.x] = s.decay[threadIdx.x];
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = s.x[tile_row(wave, r) * kPitch + at + e] * s.beta[at + e];
-      store_frag<F32, kStatePlanes>(head + (size_t)(first_frag(wave) + ks) * kPiecesOf<F32, kStatePlanes> * space.kPiece, lane, x);
+      store_frag<F32, kPlanes>(head + (size_t)(first_frag(wave) + ks) * kPiecesOf<F32, kPlanes> * space.kPiece, lane, x);
     }
   }
 }
@@ -372,11 +372,10 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
 // neighbouring columns of a token.
 template <bool F32, int DK, int NT>
 struct StateLds {
-  static constexpr int kPieces = kStatePlanes, kOutPieces = F32 ? kStatePlanes : kOutPlanes;
-  static constexpr size_t kFrag = (size_t)kPieces * kWave * 16, kOutFrag = (size_t)kOutPieces * kWave * 16;
+  static constexpr size_t kFrag = (size_t)kPlanes * kWave * 16;
   static constexpr int kStateFrags = DK / 32 * NT, kRowFrags = 2 * NT;
   // H, V - G o (K H), D_63 o U, U
-  static constexpr size_t kBytes = (kStateFrags + 2 * kRowFrags) * kFrag + kRowFrags * kOutFrag;
+  static constexpr size_t kBytes = (kStateFrags + 3 * kRowFrags) * kFrag;
 };
 
 // half `half` (4 of 8 values) of a lane's operand
@@ -446,8 +445,8 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
   using L = StateLds<F32, DK, NT>;
   using Piece = typename Frag<F32, 1>::Piece;
   constexpr int kKs = DK / 32, kTiles = DK / 64, w = sizeof(T);
-  constexpr int kKeyPieces = kPiecesOf<F32, 1>, kStatePieces = kPiecesOf<F32, kStatePlanes>, kOutPieces = kPiecesOf<F32, kOutPlanes>;
-  constexpr int kActs = F32 ? 3 : 1, kOuts = L::kOutPieces;  // planes of an activation, and for outputs
+  constexpr int kKeyPieces = kPiecesOf<F32, 1>, kSolvePieces = kPiecesOf<F32, kPlanes>, kMixPieces = kPiecesOf<true, kPlanes>;
+  constexpr int kActs = F32 ? 3 : 1;  // planes of an activation
   constexpr int kParts = NT == 1 ? 3 : 1, kOutParts = NT == 1 ? 2 : 1;
   constexpr bool kTouch = kWavesPerSimd<F32, DK, NT> == 2;
   constexpr bool kTwoSets = NT == 1 && DK <= (F32 ? 64 : 128);
@@ -511,7 +510,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       v_off[n] = col[n] < a.dv ? (uint32_t)(tile_row(wave, 4 * g) * (int)a.v_stride + col[n]) * w : kNowhere;
     struct Operands {
       Frag<F32, 1> kf[kKs], key[kTiles][2];
-      Frag<F32, kStatePlanes> ts[2];
+      Frag<F32, kPlanes> ts[2];
       uint32_t vr[NT][4];
       f32x4 gr, gu;  // decays of the rows 4 g + i, and behind them
       float gc;      // of the whole chunk
@@ -544,8 +543,8 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int j = 0; j < kStatePieces; ++j)
-          x.ts[ks].p[j] = load_piece<Piece>(ks ? more : head, lane * 16 + j * kPiece, (t0 + ks) * kStatePieces * kPiece);
+        for (int j = 0; j < kSolvePieces; ++j)
+          x.ts[ks].p[j] = load_piece<Piece>(ks ? more : head, lane * 16 + j * kPiece, (t0 + ks) * kSolvePieces * kPiece);
     };
     auto load_keys = [&](Operands &x, rsrc_t rs) {
 #pragma unroll
@@ -559,13 +558,13 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
     auto put_state = [&](int m) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
-        put_half<kStatePlanes>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
+        put_half<kPlanes>(lds_h + (size_t)((wave + 4 * m) / 2 * NT + n) * L::kFrag, half, lane, H[m][n]);
     };
 
     // One chunk, from the operands `x`; the next one's go to `y`.  Where registers
     // allow two sets, the loads lie between the products, a whole chunk ahead;
     // else they follow the last use of their registers.
-    constexpr int kKeyLoads = 2 * kTiles * kKeyPieces, kRowLoads = kKs * kKeyPieces + 4 * NT + 1, kSolveLoads = 2 * kStatePieces + 2;
+    constexpr int kKeyLoads = 2 * kTiles * kKeyPieces, kRowLoads = kKs * kKeyPieces + 4 * NT + 1, kSolveLoads = 2 * kSolvePieces + 2;
     auto step = [&](int c, Operands &x, Operands &y) {
       lds_barrier();
       const rsrc_t head = head_rows.next(c + 1), keys = key_rows.next(c + 1);
@@ -576,12 +575,12 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            sum[n].template add<kActs, kStatePlanes>(planes(x.kf[ks]), get_frag<kStatePlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane));
+            sum[n].template add<kActs, kPlanes>(planes(x.kf[ks]), get_frag<kPlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane));
         if (kTwoSets) {
           load_k(y, keys);
           load_v(y, c + 1, head);
         }
-        pace<kAhead, L::kPieces, kMfma<F32, 3>, kKs * NT, kTwoSets ? kRowLoads : 0>();
+        pace<kAhead, kPlanes, kMfma<F32, 3>, kKs * NT, kTwoSets ? kRowLoads : 0>();
         __builtin_amdgcn_sched_barrier(0);
         if (!kTwoSets) load_k(y, keys);
 #pragma unroll
@@ -596,7 +595,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
           const float v = __uint_as_float(F32 ? x.vr[n][i] : x.vr[n][i] << 16);
           u[n][i] = DELTA ? __builtin_fmaf(-x.gr[i], u[n][i], v) : v;
         }
-        if (DELTA) put_half<kStatePlanes>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, u[n]);
+        if (DELTA) put_half<kPlanes>(lds_r + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, u[n]);
       }
       if (!kTwoSets) load_v(y, c + 1, head);
       if constexpr (DELTA) {
@@ -606,12 +605,12 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            sum[n].template add<kStatePlanes, kStatePlanes>(planes(x.ts[ks]), get_frag<kStatePlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane));
+            sum[n].template add<kPlanes, kPlanes>(planes(x.ts[ks]), get_frag<kPlanes>(lds_r + (size_t)(ks * NT + n) * L::kFrag, lane));
         if (kTwoSets) {
           load_matrix(y, head);
           load_decay(y, head);
         }
-        pace<2, L::kPieces, 6, 2 * NT, kTwoSets ? kSolveLoads : 0>();
+        pace<2, kPlanes, 6, 2 * NT, kTwoSets ? kSolveLoads : 0>();
         __builtin_amdgcn_sched_barrier(0);
         if (!kTwoSets) load_matrix(y, head);
 #pragma unroll
@@ -621,8 +620,8 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        put_half<kStatePlanes>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, x.gu * u[n]);
-        put_half<kOuts>(lds_o + (size_t)(wave / 2 * NT + n) * L::kOutFrag, half, lane, u[n]);
+        put_half<kPlanes>(lds_u + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, x.gu * u[n]);
+        put_half<kPlanes>(lds_o + (size_t)(wave / 2 * NT + n) * L::kFrag, half, lane, u[n]);
       }
       const float whole = x.gc;
       if (!kTwoSets) load_decay(y, head);
@@ -636,12 +635,12 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const Frag<false, kStatePlanes> uf = get_frag<kStatePlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
+          const Frag<false, kPlanes> uf = get_frag<kPlanes>(lds_u + (size_t)(ks * NT + n) * L::kFrag, lane);
 #pragma unroll
-          for (int m = 0; m < kTiles; ++m) next[m][n].template add<kActs, kStatePlanes>(planes(x.key[m][ks]), uf);
+          for (int m = 0; m < kTiles; ++m) next[m][n].template add<kActs, kPlanes>(planes(x.key[m][ks]), uf);
         }
       if (kTwoSets) load_keys(y, keys);
-      pace<2, L::kPieces, kTiles * kMfma<F32, 3>, 2 * NT, kTwoSets ? kKeyLoads : 0>();
+      pace<2, kPlanes, kTiles * kMfma<F32, 3>, 2 * NT, kTwoSets ? kKeyLoads : 0>();
       __builtin_amdgcn_sched_barrier(0);
       if (!kTwoSets) load_keys(y, keys);
 #pragma unroll
@@ -691,7 +690,7 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
     T *out = static_cast<T *>(a.out) + ((size_t)(start + token) * a.H + h) * a.dv + slab * 16 * NT + (NT == 1 ? 4 : 8) * g;
     const size_t out_step = (size_t)kChunk * a.H * a.dv;
     Frag<F32, 1> qf[kKs];
-    Frag<F32, kOutPlanes> to[2];
+    Frag<true, kPlanes> to[2];
     float gq;  // decay of the token
     auto load_q = [&](int c) {
       const rsrc_t rs = key_rows.next(c);
@@ -706,9 +705,9 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int j = 0; j < kOutPieces; ++j)
-          to[ks].p[j] = load_piece<Piece>(ks ? more : rs, lane * 16 + j * kPiece,
-                                          ChunkSpace<F32, DK>::kSolve + (t0 + ks) * kOutPieces * kPiece);
+        for (int j = 0; j < kMixPieces; ++j)
+          to[ks].p[j] = load_piece<f32x4>(ks ? more : rs, lane * 16 + j * kPiece,
+                                          ChunkSpace<F32, DK>::kSolve + (t0 + ks) * kMixPieces * kPiece);
       gq = buf_load_f32<kPolicyDefault>(rs, token * 4, kDecay);
     };
     // Where one workgroup has a CU, nothing else runs while its loads take their time.
@@ -741,25 +740,28 @@ __global__ __launch_bounds__(kStateThreads) __attribute__((amdgpu_waves_per_eu(k
       for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          sum[n].template add<kOuts, kActs>(get_frag<kOuts>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane), planes(qf[ks]));
-      pace<kAhead, kOuts, kMfma<F32, 2>, kKs * NT>();
+          sum[n].template add<kPlanes, kActs>(get_frag<kPlanes>(lds_h + (size_t)(ks * NT + n) * L::kFrag, lane), planes(qf[ks]));
+      pace<kAhead, kPlanes, kMfma<F32, 3>, kKs * NT>();
       __builtin_amdgcn_sched_barrier(0);
-      load_q(c + 1);
       if (DELTA) lds_barrier();
+      load_q(c + 1);
+      const Frag<false, kPlanes> mix[2] = {planes(to[0]), planes(to[1])};  // while the others make the corrected values
+      const float since = gq;
+      __builtin_amdgcn_sched_barrier(0);
+      load_matrix(c + 1);
       lds_barrier();
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int i = 0; i < kOutParts; ++i) sum[n].s[i] *= gq;
+        for (int i = 0; i < kOutParts; ++i) sum[n].s[i] *= since;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          sum[n].template add<kOuts, kOuts>(get_frag<kOuts>(lds_o + (size_t)(ks * NT + n) * L::kOutFrag, lane), planes(to[ks]));
+          sum[n].template add<kPlanes, kPlanes>(get_frag<kPlanes>(lds_o + (size_t)(ks * NT + n) * L::kFrag, lane), mix[ks]);
       f32x4 o[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n) o[n] = sum[n].total();
-      load_matrix(c + 1);
       touch(c + 2);
       if (token < len - c * kChunk) {
         if constexpr (NT == 1) {

@@ -21,6 +21,8 @@ constexpr int kChunk = 64;  // tokens of a chunk: four row tiles, one to a wave
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
 
 // index of row `r` of tile `t`
 __host__ __device__ constexpr int tile_row(int t, int r) { return 32 * (t / 2) + 8 * (r / 4) + 4 * (t % 2) + r % 4; }
@@ -41,26 +43,34 @@ struct Frag<true, N> {
 template <bool F32, int N>
 constexpr int kPiecesOf = F32 ? 2 : N;
 
-// The bf16 planes of 4 values: the leading 8 bits of each, the next 8, the last
-// 8 (cut, not rounded: three planes are the value itself, and a mask and a
-// subtraction cost less than a conversion).
+// two values to one word, in one instruction
+__device__ __forceinline__ uint32_t round_pair(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
+}
+
+// The bf16 planes of 4 values: each the rest of the ones before it, rounded to
+// nearest, so that a rest is half a step at most and of either sign.  Three planes are
+// the value itself: it has 24 bits, and a rest's sign is one.  (The first plane of 3.3961e38
+// or more is infinite.  Holding it below cost 2 to 7% of the second kernel's time.)
 template <int N>
 __device__ __forceinline__ void split4(const float (&x)[4], uint2 (&p)[N]) {
-  uint32_t r[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(x[i]);
+  float r[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    p[n] = make_uint2(__builtin_amdgcn_perm(r[1], r[0], 0x07060302u), __builtin_amdgcn_perm(r[3], r[2], 0x07060302u));
-    if (n + 1 < N)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) - __uint_as_float(r[i] & 0xffff0000u));
+    p[n] = make_uint2(round_pair(r[0], r[1]), round_pair(r[2], r[3]));
+    if (n + 1 < N) {
+      r[0] -= __uint_as_float(p[n].x << 16);
+      r[1] -= __uint_as_float(p[n].x & 0xffff0000u);
+      r[2] -= __uint_as_float(p[n].y << 16);
+      r[3] -= __uint_as_float(p[n].y & 0xffff0000u);
+    }
   }
 }
 
 // An operand of the second kernel as bf16 planes.  Six products of those of fp32 values
-// take 96 cycles where eight fp32 instructions take 256, and leave out 2^-24 of a
-// product's size at most, as a rounding of it would.
+// take 96 cycles where eight fp32 instructions take 256.  Planes of 1 <= |x| < 2 are
+// 1, 2^-8 and 2^-17 at most, so the three products left out are 2 2^-25 + 2^-34 of a
+// product's size at most, as a rounding of it would be.
 template <int N>
 __device__ __forceinline__ const Frag<false, N> &planes(const Frag<false, N> &f) { return f; }
 template <int N>
@@ -75,9 +85,9 @@ __device__ __forceinline__ Frag<false, 3> planes(const Frag<true, N> &f) {
   return s;
 }
 
-// A sum of products a b of the first NA and NB planes, those of 2^-8 max(NA, NB)
-// and less of the whole left out.  It is held in S parts, by the products' size: a
-// matrix instruction waits for the one before it on the same registers.
+// A sum of products a b of NA and NB planes, those past the max(NA, NB) largest sizes
+// left out.  It is held in S parts, by the products' size: a matrix instruction waits
+// for the one before it on the same registers.
 template <int S>
 struct Sum {
   f32x4 s[S];
@@ -111,17 +121,18 @@ struct Sum {
   }
 };
 
-// Planes of what the state depends on, and of what outputs alone do that are rounded
-// to bf16.
-constexpr int kStatePlanes = 3, kOutPlanes = 2;
+// Planes of an fp32 value.  Outputs that are rounded to bf16 take all three as well:
+// with two of them they would differ in the last bit from those of fp32 products.
+constexpr int kPlanes = 3;
 
 // Row tile t of the lower triangular 64 x 64 matrices has the inner 32s ks <= t / 2.
 __host__ __device__ constexpr int first_frag(int t) { return t < 2 ? t : 2 * t - 2; }
 constexpr int kTriFrags = 6;
 
 // What the first kernel leaves, operand by operand, 16 bytes a lane:
-//   for every (slot, head): X beta and the decayed Q K^T, [6][pieces][64 lanes], and
-//   the decays G and D_63, fp32 [2][64];
+//   for every (slot, head): X beta, [6][pieces][64 lanes], the decayed Q K^T, fp32
+//   [6][2][64 lanes] (planes would be a third more bytes, and each is cut once a
+//   workgroup), and the decays G and D_63, fp32 [2][64];
 //   for every (slot, key head): K^T [d_k / 16][2][pieces][64 lanes], and K and Q
 //   [4][d_k / 32][pieces][64 lanes].  Keys and queries lie one token a row, often a
 //   power of two apart, so that a head's rows all fall to one channel of the L2; the
@@ -138,8 +149,8 @@ struct Walk {
 template <bool F32, int DK>
 struct ChunkSpace {
   static constexpr size_t kPiece = 64 * 16;
-  static constexpr size_t kSolve = kTriFrags * kPiecesOf<F32, kStatePlanes> * kPiece;
-  static constexpr size_t kMix = kTriFrags * kPiecesOf<F32, kOutPlanes> * kPiece;
+  static constexpr size_t kSolve = kTriFrags * kPiecesOf<F32, kPlanes> * kPiece;
+  static constexpr size_t kMix = kTriFrags * kPiecesOf<true, kPlanes> * kPiece;
   static constexpr size_t kDecay = kSolve + kMix, kRest = kDecay + kChunk * 4;
   static constexpr size_t kHead = kRest + kChunk * 4;
   static constexpr size_t kRows = 4 * (DK / 32) * kPiecesOf<F32, 1> * kPiece;  // of K, of Q, and of K^T
