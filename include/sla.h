@@ -595,7 +595,9 @@ int sla_prefill(const sla_prefill_shape *shape, const float *state, const void *
                 const float *beta, const int32_t *seq_start, void *out, float *state_out, void *workspace,
                 size_t workspace_bytes, int32_t *status, hipStream_t stream);
 
-/* Bytes of sla_prefill's workspace for this shape (0 on a bad shape). */
+/* Bytes of sla_prefill's workspace for this shape (0 on a bad shape).  They do not
+ * fall as tokens or batch grow: a workspace for the largest call serves smaller ones
+ * of the same heads. */
 size_t sla_prefill_workspace_bytes(const sla_prefill_shape *shape);
 
 typedef struct sla_conv_prefill_shape {

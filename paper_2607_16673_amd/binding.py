@@ -456,8 +456,9 @@ def sla_page_copy(k_cache, v_cache, src, dst, *, rows=None, status=None):
 
 # --------------------------------------------- the prompt pass of a layer
 def prefill_workspace(q, v, batch: int, *, family: str = "gdn"):
-    """A workspace for sla_prefill calls with these shapes and so many sequences
-    (None if they need none).  One call uses it at a time."""
+    """A workspace for sla_prefill calls with these shapes and so many sequences, or
+    with fewer tokens or sequences (None if they need none).  One call uses it at a
+    time."""
     nbytes = (_nat or native()).prefill_workspace_bytes(q, v, batch, FAMILIES[family])
     return _torch().empty(nbytes, dtype=_torch().uint8, device=q.device) if nbytes else None
 

@@ -10,6 +10,7 @@
 // one write of the state bound it for sequences of a token (256 of 16 heads of 128 x
 // 256: 212 us, 5.1 TB/s, the rate of a large copy), the chain of exchanges (1.2 us a
 // token where the chip is not full) for longer ones.
+#include <algorithm>
 #include <type_traits>
 
 #include "prefill_chunk.hpp"
@@ -149,12 +150,27 @@ hipError_t launch_serial(const PrefillArgs &a, hipStream_t s) {
 // 3 us.  So where all tokens together are few enough for one sequence, one launch does;
 // where an average sequence is long (few workgroups: longer than the limit; many: 64
 // tokens) all go in chunks, and short ones among them cost little beside the others.
+constexpr int kFewSerial = 6, kManySerial = 24, kManyAverage = 64;
+// workgroups of a sequence, and the batches whose workgroups fill the chip
+int64_t workgroups_of(const PrefillArgs &a) { return (int64_t)a.H * ((a.dv + kCols - 1) / kCols); }
+int64_t filling_batch() { return 4 * device_cus(); }
+
 PrefillArgs divided(PrefillArgs a) {
-  const int64_t workgroups = (int64_t)a.rows.B * a.H * ((a.dv + kCols - 1) / kCols);
-  const bool fills = workgroups >= 4 * device_cus();
-  a.serial_len = fills ? 24 : 6;
-  if (a.rows.tokens > (fills ? 64 : 6) * (int64_t)a.rows.B) a.serial_len = -1;
+  const bool fills = a.rows.B * workgroups_of(a) >= filling_batch();
+  a.serial_len = fills ? kManySerial : kFewSerial;
+  if (a.rows.tokens > (fills ? kManyAverage : kFewSerial) * (int64_t)a.rows.B) a.serial_len = -1;
   return a;
+}
+
+// Sequences in chunks that a call of up to so many tokens and sequences can have: the
+// most of the three divisions of its work, so that a workspace for the largest call
+// serves all smaller ones, whichever way they go.
+int64_t most_chunked(const PrefillArgs &a) {
+  const int64_t T = a.rows.tokens, B = a.rows.B;
+  const int64_t few = (filling_batch() - 1) / workgroups_of(a);  // the largest batch that does not fill the chip
+  const int64_t all_of_few = T > 0 ? (T - 1) / kFewSerial : 0;   // ... all of it in chunks, or those past the limit
+  const int64_t many = T / (kManySerial + 1);                    // as many as are all in chunks (T > 64 B), or more
+  return std::min(B, std::max(many, std::min(few, all_of_few)));
 }
 bool all_serial(const PrefillArgs &a) { return a.rows.tokens <= a.serial_len; }
 
@@ -178,20 +194,20 @@ hipError_t launch_t(const PrefillArgs &a, hipStream_t s) {
 }
 
 template <bool F32>
-size_t bytes_t(const PrefillArgs &a) {
+size_t bytes_t(const PrefillArgs &a, size_t slots, size_t walks) {
   switch (a.dk) {
-    case 64: return chunk_space<F32, 64>(a).bytes();
-    case 128: return chunk_space<F32, 128>(a).bytes();
-    default: return chunk_space<F32, 256>(a).bytes();
+    case 64: return ChunkSpace<F32, 64>{nullptr, slots, walks, a.H, a.Hk}.bytes();
+    case 128: return ChunkSpace<F32, 128>{nullptr, slots, walks, a.H, a.Hk}.bytes();
+    default: return ChunkSpace<F32, 256>{nullptr, slots, walks, a.H, a.Hk}.bytes();
   }
 }
 
 }  // namespace
 
-size_t prefill_workspace_bytes(const PrefillArgs &args, int dtype) {
-  const PrefillArgs a = divided(args);
-  if (all_serial(a)) return 0;
-  return dtype == SLA_DTYPE_BF16 ? bytes_t<false>(a) : bytes_t<true>(a);
+size_t prefill_workspace_bytes(const PrefillArgs &a, int dtype) {
+  const size_t walks = (size_t)most_chunked(a), slots = (size_t)(a.rows.tokens / kChunk) + walks;
+  if (walks == 0) return 0;  // fewer tokens than any sequence in chunks has
+  return dtype == SLA_DTYPE_BF16 ? bytes_t<false>(a, slots, walks) : bytes_t<true>(a, slots, walks);
 }
 
 hipError_t launch_prefill(const PrefillArgs &a, int dtype, hipStream_t s) {
