@@ -174,6 +174,40 @@ int64_t most_chunked(const PrefillArgs &a) {
 }
 bool all_serial(const PrefillArgs &a) { return a.rows.tokens <= a.serial_len; }
 
+// Slots of the workspace.  All chunks of a call at once take 20 to 100 KB a token, so
+// past kMostBytes, or eight times the states where that is more, a call goes in passes:
+// each takes some chunks of every sequence that has any left, from the states that the
+// pass before has written to state_out.
+constexpr int64_t kMostBytes = 2ll << 30;
+int64_t workspace_slots(const PrefillArgs &a, size_t of_slot) {
+  const int64_t walks = most_chunked(a), all = a.rows.tokens / kChunk + walks;
+  const int64_t states = (int64_t)a.rows.B * a.H * a.dk * a.dv * 4;
+  return std::min(all, std::max(walks, std::max(kMostBytes, 8 * states) / (int64_t)of_slot));
+}
+
+// The chunks in one pass, or in several.  The lengths are on the device: the host goes by
+// how many sequences can have more than the chunks that are done, so passes grow as
+// fewer can, and there are 1 + ln(B) times as many as evenly long sequences fill; the
+// others look at the longest sequence and end.
+template <bool F32, int DK>
+hipError_t launch_passes(PrefillArgs a, hipStream_t s) {
+  const int64_t slots = workspace_slots(a, ChunkSpace<F32, DK>::of_slot(a.H, a.Hk));
+  if (chunk_slots<kChunk>(a.rows, a.serial_len) <= slots) return launch_chunks<F32, DK>(a, s);
+  const int64_t most = (a.rows.tokens + kChunk - 1) / kChunk;  // chunks of a sequence
+  for (int64_t left = most; left > 0; left -= a.window) {
+    a.done = (int32_t)(most - left);
+    if (a.done > 0) {
+      a.serial_len = a.done * kChunk;
+      a.state = a.state_out;
+    }
+    const int64_t longer = most_longer(a.rows, a.serial_len);
+    a.window = (int32_t)std::min(left, slots / longer);
+    const hipError_t e = launch_chunks<F32, DK>(a, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <bool F32, int DK>
 hipError_t launch_dk(const PrefillArgs &a, hipStream_t s) {
   using T = typename std::conditional<F32, float, bf16>::type;
@@ -181,7 +215,7 @@ hipError_t launch_dk(const PrefillArgs &a, hipStream_t s) {
     const hipError_t e = launch_serial<T, DK>(a, s);
     if (e != hipSuccess || all_serial(a)) return e;
   }
-  return launch_chunks<F32, DK>(a, s);
+  return launch_passes<F32, DK>(a, s);
 }
 
 template <bool F32>
@@ -193,21 +227,25 @@ hipError_t launch_t(const PrefillArgs &a, hipStream_t s) {
   }
 }
 
+template <bool F32, int DK>
+size_t bytes_dk(const PrefillArgs &a) {
+  using Space = ChunkSpace<F32, DK>;
+  return Space{nullptr, (size_t)workspace_slots(a, Space::of_slot(a.H, a.Hk)), (size_t)most_chunked(a), a.H, a.Hk}.bytes();
+}
 template <bool F32>
-size_t bytes_t(const PrefillArgs &a, size_t slots, size_t walks) {
+size_t bytes_t(const PrefillArgs &a) {
   switch (a.dk) {
-    case 64: return ChunkSpace<F32, 64>{nullptr, slots, walks, a.H, a.Hk}.bytes();
-    case 128: return ChunkSpace<F32, 128>{nullptr, slots, walks, a.H, a.Hk}.bytes();
-    default: return ChunkSpace<F32, 256>{nullptr, slots, walks, a.H, a.Hk}.bytes();
+    case 64: return bytes_dk<F32, 64>(a);
+    case 128: return bytes_dk<F32, 128>(a);
+    default: return bytes_dk<F32, 256>(a);
   }
 }
 
 }  // namespace
 
 size_t prefill_workspace_bytes(const PrefillArgs &a, int dtype) {
-  const size_t walks = (size_t)most_chunked(a), slots = (size_t)(a.rows.tokens / kChunk) + walks;
-  if (walks == 0) return 0;  // fewer tokens than any sequence in chunks has
-  return dtype == SLA_DTYPE_BF16 ? bytes_t<false>(a, slots, walks) : bytes_t<true>(a, slots, walks);
+  if (most_chunked(a) == 0) return 0;  // fewer tokens than any sequence in chunks has
+  return dtype == SLA_DTYPE_BF16 ? bytes_t<false>(a) : bytes_t<true>(a);
 }
 
 hipError_t launch_prefill(const PrefillArgs &a, int dtype, hipStream_t s) {

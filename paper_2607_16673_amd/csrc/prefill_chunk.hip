@@ -112,17 +112,25 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
   const unsigned slot = wg / (unsigned)a.H;
   const int h = (int)(wg % (unsigned)a.H), group = a.H / a.Hk, kh = h / group;
   if (slot >= space.slots) return;
+  if (a.done > 0 && slot > 0 && *space.longest() <= a.done * kChunk) return;  // a pass that no sequence reaches
   bool ok;
-  const Chunk c = find_chunk<kChunk>(a.rows, a.serial_len, (int)slot, lane, ok);
+  const Chunk c = find_chunk<kChunk>(a.rows, a.serial_len, (int)slot, lane, ok, a.window, a.done);
   if (h == 0) {
     if (!ok && a.status)
       for (int64_t i = (int64_t)slot * kThreads + threadIdx.x; i < a.rows.B; i += (int64_t)space.slots * kThreads)
         a.status[i] = SLA_ERR_LENGTH;
     if (slot == 0 && threadIdx.x == 0) *space.walk_count() = ok ? c.longer : -1;
+    if (slot == 0 && wave == 0 && a.window && a.done == 0) {  // for the passes behind this one
+      int longest = 0;
+      for (int i = lane; ok && i < a.rows.B; i += kWave) longest = max(longest, a.rows.start[i + 1] - a.rows.start[i]);
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) longest = max(longest, __shfl_xor(longest, o));
+      if (lane == 0) *space.longest() = longest;
+    }
     if (c.b >= 0 && c.first && wave == 0) {
       const int place = a.rows.B <= kWave ? place_by_length(a.rows, c.b, lane) : c.rank;
       if (lane == 0) {
-        *space.walk(place) = Walk{c.b, c.row, a.rows.start[c.b + 1] - c.row, c.row / kChunk + c.rank};
+        *space.walk(place) = Walk{c.b, c.row, a.window ? min(c.left, a.window * kChunk) : c.left, (int)slot};
         if (a.status) a.status[c.b] = SLA_OK;
       }
     }
@@ -806,7 +814,7 @@ hipError_t launch_family(const PrefillArgs &a, hipStream_t s) {
   const auto first = matrices_kernel<F32, DK, DELTA>;
   hipError_t e = allow_lds(first, sizeof(M));
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(first, grid_of((uint64_t)chunk_slots<kChunk>(a.rows, a.serial_len) * a.H), dim3(kThreads), sizeof(M), s, a);
+  hipLaunchKernelGGL(first, grid_of((uint64_t)chunk_slots<kChunk>(a.rows, a.serial_len, a.window) * a.H), dim3(kThreads), sizeof(M), s, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   // 16 columns of a state to a workgroup where 32 leave half of the CUs without one

@@ -139,15 +139,17 @@ constexpr int kTriFrags = 6;
 //   workgroups of a head that read them chunk by chunk would wait there for one
 //   another (one sequence of 32768 tokens, 16 heads: the second kernel 998 us, 830 with
 //   them laid out, the first 30 longer).
-//   and behind them which sequences the second walks, the longest first in batches of
-//   up to 64, so that no long one is begun when the others have ended: their number
-//   (-1: bad starts), then one of these each.
+//   behind them which sequences the second walks, the longest first in batches of up to
+//   64, so that no long one is begun when the others have ended;
+//   and in front of them, where every pass of a call finds them, the number of these
+//   (-1: bad starts) and the tokens of the longest sequence.
 struct Walk {
   int32_t b, start, len, slot;
 };
 
 template <bool F32, int DK>
 struct ChunkSpace {
+  static constexpr size_t kFront = 128;  // a line, so that the operands begin with one
   static constexpr size_t kPiece = 64 * 16;
   static constexpr size_t kSolve = kTriFrags * kPiecesOf<F32, kPlanes> * kPiece;
   static constexpr size_t kMix = kTriFrags * kPiecesOf<true, kPlanes> * kPiece;
@@ -155,22 +157,27 @@ struct ChunkSpace {
   static constexpr size_t kHead = kRest + kChunk * 4;
   static constexpr size_t kRows = 4 * (DK / 32) * kPiecesOf<F32, 1> * kPiece;  // of K, of Q, and of K^T
   static constexpr size_t kKeys = 3 * kRows;
+  static size_t of_slot(int H, int Hk) { return H * kHead + Hk * kKeys; }
 
   unsigned char *base;
   size_t slots, walks;
   int H, Hk;
 
   __host__ __device__ size_t operands() const { return slots * (H * kHead + Hk * kKeys); }
-  __host__ __device__ size_t bytes() const { return operands() + (walks + 1) * sizeof(Walk); }
-  __device__ int32_t *walk_count() const { return reinterpret_cast<int32_t *>(base + operands()); }
-  __device__ Walk *walk(int i) const { return reinterpret_cast<Walk *>(base + operands()) + 1 + i; }
-  __device__ unsigned char *head(size_t slot, int h) const { return base + (slot * H + h) * kHead; }
-  __device__ unsigned char *keys(size_t slot, int kh) const { return base + slots * H * kHead + (slot * Hk + kh) * kKeys; }
+  __host__ __device__ size_t walk_at(size_t i) const { return kFront + operands() + i * sizeof(Walk); }
+  __host__ __device__ size_t bytes() const { return walk_at(walks); }
+  __device__ int32_t *walk_count() const { return reinterpret_cast<int32_t *>(base); }
+  __device__ int32_t *longest() const { return walk_count() + 1; }
+  __device__ Walk *walk(int i) const { return reinterpret_cast<Walk *>(base + walk_at(i)); }
+  __host__ __device__ unsigned char *head(size_t slot, int h) const { return base + kFront + (slot * H + h) * kHead; }
+  __host__ __device__ unsigned char *keys(size_t slot, int kh) const {
+    return base + kFront + slots * H * kHead + (slot * Hk + kh) * kKeys;
+  }
 };
 
 template <bool F32, int DK>
 __host__ __device__ inline ChunkSpace<F32, DK> chunk_space(const PrefillArgs &a) {
-  return {static_cast<unsigned char *>(a.workspace), (size_t)chunk_slots<kChunk>(a.rows, a.serial_len),
+  return {static_cast<unsigned char *>(a.workspace), (size_t)chunk_slots<kChunk>(a.rows, a.serial_len, a.window),
           (size_t)most_longer(a.rows, a.serial_len), a.H, a.Hk};
 }
 

@@ -22,6 +22,7 @@ struct PrefillArgs {
   int32_t H, Hk, dk, dv;
   int32_t family;
   int32_t serial_len;    // sequences up to this length go token by token, longer ones in chunks (-1: all in chunks)
+  int32_t window, done;  // a pass of the chunked kernels takes so many chunks of each sequence, behind so many (0: all)
   const float *state;    // [B][H][dk][dv] or null
   const void *q, *k, *v;
   int64_t q_stride, k_stride, v_stride;  // elements from row to row

@@ -24,10 +24,15 @@ __host__ __device__ inline int64_t most_longer(const PackedRows &r, int min_len)
 // having one empty chunk).  Chunk c of sequence b has the slot start[b] / C + rank + c,
 // rank counting the longer sequences before b: ceil(len / C) <= end / C - start / C + 1,
 // so no two share one, and no table of chunk counts has to be summed up first.  Some
-// slots stay empty.
+// slots stay empty.  With a window of w chunks, those behind the first `done`, chunk
+// done + c has the slot w rank + c.
 template <int C>
-__host__ __device__ inline int64_t chunk_slots(const PackedRows &r, int min_len) {
-  return (int64_t)r.tokens / C + most_longer(r, min_len);
+__host__ __device__ inline int64_t chunk_slots(const PackedRows &r, int min_len, int window = 0) {
+  return window ? most_longer(r, min_len) * window : (int64_t)r.tokens / C + most_longer(r, min_len);
+}
+template <int C>
+__host__ __device__ inline int first_slot(int start, int rank, int window = 0) {
+  return window ? rank * window : start / C + rank;
 }
 
 // Whether the starts are in order and inside the rows (wave-uniform).  Every wave
@@ -53,42 +58,55 @@ struct Chunk {
   int b;      // sequence, -1: none
   int row;    // first row
   int rows;   // 1..C, 0: the one chunk of an empty sequence
-  bool first;
-  int rank;    // longer sequences before its own
-  int longer;  // longer sequences in all
+  int left;   // the sequence's rows from `row` on
+  bool first; // of the sequence (of its window)
+  int rank;   // longer sequences before its own
+  int longer; // longer sequences in all
 };
 
-// The chunk of a slot (wave-uniform): its sequence is the last whose first slot is
-// not behind it.  `ok` says whether the starts are in order.
+// The chunk of slot `slot`, from the sequence whose first slot is the last not behind
+// it: its rows [start, end), that slot `front`, its rank.
 template <int C>
-__device__ __forceinline__ Chunk find_chunk(const PackedRows &r, int min_len, int slot, int lane, bool &ok) {
+__host__ __device__ inline void chunk_at(Chunk &c, int slot, int b, int start, int end, int front, int rank, int window, int done) {
+  const int at = slot - front;
+  if (window && at >= window) return;
+  const int64_t row = start + (int64_t)(done + at) * C;
+  if (at > 0 && row >= end) return;
+  c.b = b;
+  c.rank = rank;
+  c.row = (int)row;
+  c.left = end - c.row;
+  c.rows = c.left < C ? c.left : C;
+  c.first = at == 0;
+}
+
+// The chunk of a slot (wave-uniform).  `ok` says whether the starts are in order.
+template <int C>
+__device__ __forceinline__ Chunk find_chunk(const PackedRows &r, int min_len, int slot, int lane, bool &ok, int window = 0,
+                                            int done = 0) {
   bool bad = false;
-  int rank = 0, b = -1, start = 0, end = 0, front = 0;
+  int longer = 0, rank = 0, b = -1, start = 0, end = 0, front = 0;
   for (int i = 0; i < r.B; i += kWave) {
     const bool live = i + lane < r.B;
     const int a = live ? r.start[i + lane] : 0, e = live ? r.start[i + lane + 1] : 0;
     bad = bad || (live && (a < 0 || a > e || e > r.tokens));
-    const uint64_t longer = __ballot(live && (int64_t)e - a > min_len);
-    const int mine = a / C + rank + __popcll(longer & ((1ull << lane) - 1));
-    const uint64_t before = __ballot(mine <= slot) & longer;
-    if (before) {
-      const int l = 63 - __builtin_clzll(before);
+    const uint64_t mask = __ballot(live && (int64_t)e - a > min_len);
+    const int before = longer + __popcll(mask & ((1ull << lane) - 1));
+    const int mine = first_slot<C>(a, before, window);
+    const uint64_t reached = __ballot(mine <= slot) & mask;
+    if (reached) {
+      const int l = 63 - __builtin_clzll(reached);
       b = i + l;
       start = __builtin_amdgcn_readlane(a, l);
       end = __builtin_amdgcn_readlane(e, l);
       front = __builtin_amdgcn_readlane(mine, l);
+      rank = __builtin_amdgcn_readlane(before, l);
     }
-    rank += __popcll(longer);
+    longer += __popcll(mask);
   }
   ok = !wave_any(bad);
-  Chunk c = {-1, 0, 0, false, 0, rank};
-  const int at = slot - front;
-  if (!ok || b < 0 || (at > 0 && (int64_t)at * C >= end - start)) return c;
-  c.b = b;
-  c.rank = front - start / C;
-  c.row = start + at * C;
-  c.rows = min(C, end - c.row);
-  c.first = at == 0;
+  Chunk c = {-1, 0, 0, 0, false, 0, longer};
+  if (ok && b >= 0) chunk_at<C>(c, slot, b, start, end, front, rank, window, done);
   return c;
 }
 
