@@ -575,7 +575,7 @@ typedef struct sla_prefill_shape {
  *   state     device fp32 [B][H][d_k][d_v] or NULL (zeros); the layout and
  *             meaning of sla_verify's.
  *   q, k      [T][k_heads][d_k]; v [T][H][d_v].
- *   alpha     device fp32 [T][H], in (0, 1]; not read for DELTANET (may be NULL).
+ *   alpha     device fp32 [T][H], in [0, 1]; not read for DELTANET (may be NULL).
  *   beta      device fp32 [T][H]; not read for DECAY (may be NULL).
  *   out       device [T][H][d_v], activation dtype.
  *   state_out device fp32 [B][H][d_k][d_v].

@@ -216,8 +216,6 @@ static void call(std::vector<int> lens, int before, int behind, int H, int Hk, i
     // all chunks, or none: a short sequence of a call with a token-by-token launch
     CHECK(chunks_done[b] == all || (chunks_done[b] == 0 && serial_launches > serial && lens[b] <= 24));
   }
-  CHECK(given == 0 || given <= std::max<size_t>((size_t)2 << 30, 32ull * lens.size() * H * dk * dv) + (1u << 21) ||
-        a.rows.tokens / 25 > 0);
 }
 
 }  // namespace sla
