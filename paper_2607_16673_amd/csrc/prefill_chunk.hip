@@ -37,19 +37,19 @@ __device__ __forceinline__ void lds_barrier() {
 // ALUs, the others from them by fp32 matrix instructions, so that no power of L, which
 // may be large where X is not, is ever formed.
 //
-// 537 chunks of 32 heads (16 key heads) of 128 take 288 us: 0.6 GB read and 0.96 GB
-// written, 5.4 TB/s, the rate of a large copy, over a chain of steps in each workgroup
-// that would take 214 us by itself (vector ALUs busy 43%, matrix cores 11%).  It took 429
-// us with three workgroups to a CU (the keys' place in LDS is now the matrices'), 360
-// with loads that waited for one another behind their bounds checks (rows are clamped
-// instead).  Heads of one key head on one XCD read half as much, and took 297.
+// 537 chunks of 32 heads (16 key heads) of 128 take 281 us: 0.6 GB read and 0.96 GB
+// written, 5.6 TB/s, the rate of a large copy, over a chain of steps in each workgroup
+// that would take 214 us by itself (vector ALUs busy 43%, matrix cores 12%).  It took 429
+// us before the matrices had the keys' place in LDS, 360 with loads that waited for one
+// another behind their bounds checks (rows are clamped instead).  Registers hold three
+// workgroups to a CU.  Heads of one key head on one XCD read half as much, and took 297.
 template <bool F32, int DK>
 struct MatricesLds {
   using T = typename std::conditional<F32, float, bf16>::type;
   static constexpr int kKeyPitch = DK + 16 / (int)sizeof(T);
   union {
     T k[kChunk * kKeyPitch];
-    float x[kChunk * kPitch];  // L, then X, when the keys have been used: six workgroups to a CU instead of three
+    float x[kChunk * kPitch];  // L, then X, when the keys have been used
   };
   float d[4][16][16];        // D inside the diagonal blocks
   float upto[kChunk];        // product of a block's gates up to i
@@ -365,15 +365,16 @@ __global__ __launch_bounds__(kThreads) void matrices_kernel(PrefillArgs a) {
 // time the first ones wait for one another: three barriers a chunk.  What comes
 // from memory is asked for as soon as the chunk before has used its registers.
 //
-// The chain of chunks bounds one long sequence: 512 chunks, 16 heads of 128, 815 us or
-// 3800 cycles a chunk, of which three products from LDS, their planes cut and put back
-// and the barriers are 2900, the rest waits for loads (870 us without `touch` below, 617
-// with every chunk's lines the same, 532 with no loads).  Many sequences are bound by LDS, matrix cores and vector ALUs in
-// turn (53, 40 and 39% busy): 32 sequences of up to 2048 tokens, 32 heads, 537 chunks
-// in 588 us with two workgroups to a CU.  Four column tiles to a workgroup take 653,
-// one takes 860.  fp32 activations are bound by the vector ALUs, busy 60%, which cut
-// operands into planes (152 chunks of 12 heads of 64 x 80 in 61 us; 80 with fp32
-// matrix instructions).
+// The chain of chunks bounds one long sequence: 512 chunks, 16 heads of 128, 842 us or
+// 3950 cycles a chunk: three products from LDS, their planes made and put back, the
+// barriers, and waits for loads (with planes that were cut, 815 us in all: 870 without
+// `touch` below, 617 with every chunk's lines the same, 532 with no loads).  Many
+// sequences are bound by LDS, vector ALUs and matrix cores in turn (59, 51 and 47%
+// busy): 32 sequences of up to 2048 tokens, 32 heads, 537 chunks in 605 us with two
+// workgroups to a CU (a tenth less with two planes for the outputs; four column tiles to
+// a workgroup and one were a tenth and half as much again slower).  fp32 activations are
+// bound by the vector ALUs, busy 64%, which cut operands into planes (152 chunks of 12
+// heads of 64 x 80 in 61 us; 80 with fp32 matrix instructions).
 //
 // Columns: lane r of column tile n has the column 32 (n / 2) + 8 (r / 4) + 4 (n % 2)
 // + r % 4 of the slab, so that an output tile, made transposed, gives each lane 8

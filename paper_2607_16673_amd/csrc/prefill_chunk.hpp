@@ -137,8 +137,8 @@ constexpr int kTriFrags = 6;
 //   [4][d_k / 32][pieces][64 lanes].  Keys and queries lie one token a row, often a
 //   power of two apart, so that a head's rows all fall to one channel of the L2; the
 //   workgroups of a head that read them chunk by chunk would wait there for one
-//   another (one sequence of 32768 tokens, 16 heads: the second kernel 998 us, 830 with
-//   them laid out, the first 30 longer).
+//   another (one sequence of 32768 tokens, 16 heads, with planes that were cut: the second
+//   kernel 998 us, 830 with them laid out, the first 30 longer).
 //   behind them which sequences the second walks, the longest first in batches of up to
 //   64, so that no long one is begun when the others have ended;
 //   and in front of them, where every pass of a call finds them, the number of these
