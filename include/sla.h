@@ -598,7 +598,7 @@ int sla_prefill(const sla_prefill_shape *shape, const float *state, const void *
 /* Bytes of sla_prefill's workspace for this shape (0 on a bad shape).  They do not
  * fall as tokens or batch grow: a workspace for the largest call serves smaller ones
  * of the same heads.  They end at the largest of 2 GiB, eight times the states, and a
- * chunk's operands (31 KB a head, 25 to 200 KB a key head) for each sequence that can
+ * chunk's operands (25 or 31 KB a head, 25 to 197 KB a key head) for each sequence that can
  * have more than 24 tokens: calls that would take more go through their sequences in
  * several passes. */
 size_t sla_prefill_workspace_bytes(const sla_prefill_shape *shape);
